@@ -1,0 +1,436 @@
+"""Operators around the experts' products, over the range of sizes that a program using the library has them in.
+
+Four operators, each through the public binding where `own` is true and in its plain form, elementary torch operations in
+32 bits, where it is not:
+  dispatch  assignments sorted by expert, and the tokens' rows brought into that order, as they are or in 8 bits
+  combine   the rows brought back into token order and summed with the gate weights; or that sum's gradient
+  quantize  values in 8 bits (e4m3) with a scale for each 128 of a row (as they are, or behind SiLU(gate) * up), or for each
+            128 x 128 of a weight matrix
+  product   each expert's rows times its weights, both in 8 bits with those scales
+
+Hidden states have unit variance (what a layer gets behind a normalisation) with a few wide columns, weights are N(0, 0.02).
+Rows behind the last assigned one are left as they were (zeros here).
+"""
+import math
+
+import torch
+
+own = False
+
+BLOCK = 128
+TOP = 448.0            # largest e4m3 value
+LEAST = 2.0 ** -100    # what a block's largest magnitude counts as at least
+F8 = torch.float8_e4m3fn
+
+
+def _pad(n):
+    return (n + BLOCK - 1) // BLOCK * BLOCK
+
+
+def _dispatch(name, T, H, E, k, fp8=False, bf16=True, resident=1.0, zipf=False):
+    return {"name": name, "op": "dispatch", "T": T, "H": H, "E": E, "k": k, "fp8": fp8, "bf16": bf16, "resident": resident,
+            "zipf": zipf}
+
+
+def _combine(name, T, H, E, k, grad=False, bf16=True, out_bf16=False, resident=1.0, zipf=False):
+    return {"name": name, "op": "combine", "T": T, "H": H, "E": E, "k": k, "grad": grad, "bf16": bf16, "out_bf16": out_bf16,
+            "resident": resident, "zipf": zipf}
+
+
+def _rows(name, M, K, swiglu=False, bf16=True):
+    return {"name": name, "op": "quantize", "of": "swiglu" if swiglu else "rows", "M": M, "K": K, "bf16": bf16}
+
+
+def _weights(name, E, N, K, bf16=True):
+    return {"name": name, "op": "quantize", "of": "weights", "E": E, "N": N, "K": K, "bf16": bf16}
+
+
+def _product(name, T, k, E, N, K, out_bf16=True, resident=1.0, zipf=False):
+    return {"name": name, "op": "product", "T": T, "k": k, "E": E, "N": N, "K": K, "out_bf16": out_bf16, "resident": resident,
+            "zipf": zipf}
+
+
+def listed():
+    return [
+        # plain decoding: one token's six assignments; launches and host work are all there is
+        _dispatch("dispatch_T1", 1, 2048, 64, 6),
+        # a short prompt at widths no tile divides, a third of the experts elsewhere, skewed routing, fp32 rows
+        _dispatch("dispatch_ragged_T1000", 1000, 2040, 60, 4, bf16=False, resident=0.65, zipf=True),
+        # a large batch of prompts, its rows in 8 bits as the products take them
+        _dispatch("dispatch_fp8_T16384", 16384, 2048, 64, 6, fp8=True),
+        # the verify step (8 draft tokens + 1) with half of the experts resident
+        _combine("combine_T9", 9, 2048, 64, 6, resident=0.5),
+        # prompts: back into token order, bf16 to bf16
+        _combine("combine_T8192", 8192, 2048, 64, 6, out_bf16=True),
+        # the gradient of that sum where the router and what lies below are tuned; wide rows
+        _combine("combine_grad_T4096", 4096, 4096, 8, 2, grad=True, out_bf16=True, zipf=True),
+        # between the two products of a prompt's experts
+        _rows("swiglu_fp8_M24576", 24576, 1408, swiglu=True),
+        # one layer's large experts, quantised as they are loaded
+        _weights("weights_fp8_8x14336x4096", 8, 14336, 4096),
+        # the verify step's gate and up rows, half of the experts resident
+        _product("product_T9", 9, 6, 64, 2816, 2048, resident=0.5),
+        # one token through two of eight large experts, down
+        _product("product_large_T1", 1, 2, 8, 4096, 14336),
+        # a batch of requests, widths that no tile divides, fp32 out, skewed routing
+        _product("product_ragged_T250", 250, 4, 40, 2040, 1000, out_bf16=False, resident=0.8, zipf=True),
+        # prompts through all experts of a layer
+        _product("product_T8192", 8192, 6, 64, 2816, 2048),
+    ]
+
+
+def _logint(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _width(rng, lo, hi):
+    step = rng.choice([128, 128, 64, 8, 8])
+    return max(step, _logint(rng, lo, hi) // step * step)
+
+
+def draw(rng):
+    most = max(work(c)["flops"] for c in listed())
+    heaviest = max(work(c)["bytes"] for c in listed())
+    while True:
+        op = rng.choice(["dispatch", "dispatch", "combine", "combine", "quantize", "product", "product", "product"])
+        E = rng.choice([4, 8, 16, 40, 60, 64, 64, 100, 128, 256])
+        k = rng.randint(1, min(8, E))
+        resident, zipf = rng.choice([1.0, 1.0, 0.75, 0.5]), rng.random() < 0.3
+        if op == "dispatch":
+            case = _dispatch("", _logint(rng, 1, 16384), _width(rng, 256, 4096), E, k, rng.random() < 0.5, rng.random() < 0.7,
+                             resident, zipf)
+        elif op == "combine":
+            case = _combine("", _logint(rng, 1, 8192), _width(rng, 256, 4096), E, k, rng.random() < 0.5, rng.random() < 0.7,
+                            rng.random() < 0.5, resident, zipf)
+        elif op == "quantize":
+            if rng.random() < 0.3:
+                case = _weights("", rng.choice([1, 4, 8, 32]), _width(rng, 256, 8192), _width(rng, 256, 8192), rng.random() < 0.7)
+            else:
+                case = _rows("", _logint(rng, 1, 32768), _width(rng, 256, 8192), rng.random() < 0.5, rng.random() < 0.7)
+        else:
+            case = _product("", _logint(rng, 1, 8192), k, E, _width(rng, 256, 8192), _width(rng, 256, 8192), rng.random() < 0.7,
+                            resident, zipf)
+            if case["E"] * case["N"] * case["K"] > 1 << 29:
+                continue
+        w = work(case)
+        if w["flops"] <= most and w["bytes"] <= heaviest:
+            del case["name"]
+            return case
+
+
+def work(case):
+    """One pass's bytes and operations.  How many assignments are resident and which experts are hit goes by the routing: their expected
+    numbers under the case's routing stand here (uniform routing; skewed routing hits fewer experts)."""
+    op = case["op"]
+    s = 2 if case.get("bf16", True) else 4
+    if op in ("dispatch", "combine"):
+        T, H, E, k = case["T"], case["H"], case["E"], case["k"]
+        A = T * k
+        V = A * case["resident"]
+        if op == "dispatch":
+            row = _pad(H) * (1 + 4 / BLOCK) if case["fp8"] else H * s
+            return {"bytes": 4 * A + T * H * s + 4 * (E + 1) + 8 * A + V * row, "flops": T * H * 3.0 if case["fp8"] else 0.0}
+        so = 2 if case["out_bf16"] else 4
+        if case["grad"]:
+            return {"bytes": T * H * so + 2 * V * H * s + 12 * A, "flops": 3.0 * V * H}
+        return {"bytes": V * H * s + T * H * so + 8 * A, "flops": 2.0 * V * H}
+    if op == "quantize":
+        if case["of"] == "weights":
+            E, N, K = case["E"], case["N"], case["K"]
+            return {"bytes": E * N * (K * s + _pad(K)) + 4 * E * _pad(N) * _pad(K) / BLOCK ** 2, "flops": 3.0 * E * N * K}
+        M, K = case["M"], case["K"]
+        n = 2 if case["of"] == "swiglu" else 1
+        return {"bytes": M * (K * s * n + _pad(K) * (1 + 4 / BLOCK)), "flops": M * K * (3.0 + (8.0 if n == 2 else 0.0))}
+    T, k, E, N, K = (case[n] for n in ("T", "k", "E", "N", "K"))
+    R, live = T * k * case["resident"], E * case["resident"]
+    hit = live * (1 - (1 - k / E) ** T) if not case["zipf"] else min(live, R)
+    so = 2 if case["out_bf16"] else 4
+    return {"bytes": R * _pad(K) * (1 + 4 / BLOCK) + hit * (N * _pad(K) + 4 * _pad(N) * _pad(K) / BLOCK ** 2) + R * N * so,
+            "flops": 2.0 * R * N * K}
+
+
+def _routing(case, g):
+    """[T,k] int32: distinct experts a token, those that are not resident as -1 (a slot lookup's result)."""
+    T, E, k = case["T"], case["E"], case["k"]
+    logits = torch.randn(T, E, generator=g, device="cuda")
+    if case["zipf"]:
+        rank = torch.randperm(E, generator=g, device="cuda").float()
+        logits = logits - 1.1 * torch.log1p(rank)
+    ids = torch.topk(logits, k, dim=1).indices.to(torch.int32)
+    if case["resident"] < 1.0:
+        gone = torch.randperm(E, generator=g, device="cuda")[: E - max(1, int(E * case["resident"]))]
+        table = torch.arange(E, dtype=torch.int32, device="cuda")
+        table[gone] = -1
+        ids = table[ids.long()]
+    return ids.contiguous()
+
+
+def _hidden(rows, width, bf16, g, std=1.0):
+    x = torch.randn(rows, width, generator=g, device="cuda") * std
+    x[:, torch.randint(0, width, (max(1, width // 256),), generator=g, device="cuda")] *= 8.0
+    return x.to(torch.bfloat16) if bf16 else x
+
+
+def _eight_bits(x, tall):
+    """(values, scales) of a matrix or a stack of them whose sizes 128 divides; blocks of 1 x 128, or 128 x 128 where `tall`."""
+    n, kb = x.shape[-2], x.shape[-1] // BLOCK
+    h = BLOCK if tall else 1
+    b = x.reshape(-1, n // h, h, kb, BLOCK)
+    m = b.abs().amax(dim=(2, 4), keepdim=True).clamp(min=LEAST)
+    q = (b * (TOP / m)).to(F8).reshape(x.shape)
+    return q, (m / TOP).reshape(*x.shape[:-2], n // h, kb)
+
+
+def _fill(shape, dtype):
+    if dtype == F8:
+        return torch.zeros(shape, dtype=torch.uint8, device="cuda").view(F8)
+    return torch.zeros(shape, dtype=dtype, device="cuda")
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    s = {"case": case}
+    op = case["op"]
+    i32 = torch.int32
+    if op in ("dispatch", "combine"):
+        T, H, E, k = case["T"], case["H"], case["E"], case["k"]
+        A = T * k
+        dtype = torch.bfloat16 if case["bf16"] else torch.float32
+        s["ids"] = _routing(case, g)
+        if op == "dispatch":
+            s["x"] = _hidden(T, H, case["bf16"], g)
+            s["offsets"], s["order"], s["pos"] = _fill((E + 1,), i32), _fill((A,), i32), _fill((T, k), i32)
+            s["rows"] = _fill((A, _pad(H) if case["fp8"] else H), F8 if case["fp8"] else dtype)
+            if case["fp8"]:
+                s["scale"] = _fill((A, _pad(H) // BLOCK), torch.float32)
+            return s
+        s["offsets"], s["order"], s["pos"] = _sorted(s["ids"], E)
+        s["rows"] = _hidden(A, H, case["bf16"], g, 0.5)
+        s["w"] = torch.softmax(torch.randn(T, k, generator=g, device="cuda"), dim=1)
+        out = torch.bfloat16 if case["out_bf16"] else torch.float32
+        if case["grad"]:
+            s["dout"] = _hidden(T, H, case["out_bf16"], g, 0.1)
+            s["drows"], s["dw"] = _fill((A, H), dtype), _fill((T, k), torch.float32)
+        else:
+            s["out"] = _fill((T, H), out)
+        return s
+    if op == "quantize":
+        if case["of"] == "weights":
+            E, N, K = case["E"], case["N"], case["K"]
+            w = torch.empty((E, N, K), dtype=torch.bfloat16 if case["bf16"] else torch.float32, device="cuda")
+            s["x"] = w.normal_(0.0, 0.02, generator=g)
+            s["q"], s["scale"] = _fill((E, N, _pad(K)), F8), _fill((E, _pad(N) // BLOCK, _pad(K) // BLOCK), torch.float32)
+            return s
+        M, K = case["M"], case["K"]
+        # (the products' outputs: gate and up of a row side by side)
+        s["x"] = _hidden(M, 2 * K if case["of"] == "swiglu" else K, case["bf16"], g)
+        s["q"], s["scale"] = _fill((M, _pad(K)), F8), _fill((M, _pad(K) // BLOCK), torch.float32)
+        return s
+    T, k, E, N, K = (case[n] for n in ("T", "k", "E", "N", "K"))
+    A, Kp, Np = T * k, _pad(K), _pad(N)
+    s["offsets"] = _sorted(_routing(case, g), E)[0]
+    a = torch.zeros((A, Kp), device="cuda")
+    a[:, :K] = _hidden(A, K, False, g)
+    s["a"], s["a_scale"] = _eight_bits(a, False)
+    q, scale = _fill((E, N, Kp), F8), _fill((E, Np // BLOCK, Kp // BLOCK), torch.float32)
+    w = torch.zeros((Np, Kp), device="cuda")
+    for e in range(E):
+        w[:N, :K].normal_(0.0, 0.02, generator=g)
+        v, scale[e] = _eight_bits(w, True)
+        q[e] = v[:N]
+    s["w"], s["w_scale"] = q, scale
+    s["out"] = _fill((A, N), torch.bfloat16 if case["out_bf16"] else torch.float32)
+    return s
+
+
+# ---- plain forms ----
+
+def _sorted(ids, E):
+    """offsets [E+1], order [A], pos [T,k] of a stable sort of the assignments by expert; ids outside [0,E) come to no row."""
+    flat = ids.reshape(-1)
+    key = torch.where((flat >= 0) & (flat < E), flat, E)
+    keys, order = torch.sort(key, stable=True)
+    offsets = torch.searchsorted(keys, torch.arange(E + 1, dtype=keys.dtype, device=keys.device)).to(torch.int32)
+    here = keys < E
+    pos = torch.empty_like(flat)
+    pos[order] = torch.where(here, torch.arange(flat.numel(), dtype=torch.int32, device=flat.device), -1)
+    return offsets, torch.where(here, order, -1).to(torch.int32), pos.reshape(ids.shape)
+
+
+def _quantized(x):
+    """(q [M,Kp], scale [M,Kp/128]) of fp32 rows of any width."""
+    M, K = x.shape
+    return _eight_bits(torch.nn.functional.pad(x, (0, _pad(K) - K)), False)
+
+
+def _plain_dispatch(s):
+    case = s["case"]
+    offsets, order, pos = _sorted(s["ids"], case["E"])
+    here = (order >= 0).unsqueeze(1)
+    token = order.clamp(min=0).long() // case["k"]
+    if case["fp8"]:
+        q, scale = _quantized(s["x"].float())
+        rows = torch.where(here, q.view(torch.uint8)[token], 0).view(F8)
+        return offsets, order, pos, rows, torch.where(here, scale[token], 0.0)
+    return offsets, order, pos, torch.where(here, s["x"][token], 0.0)
+
+
+def _plain_combine(s):
+    T, k = s["pos"].shape
+    here = (s["pos"] >= 0).unsqueeze(2)
+    picked = torch.where(here, s["rows"].float()[s["pos"].clamp(min=0).long()], 0.0)
+    if not s["case"]["grad"]:
+        return (picked * s["w"].unsqueeze(2)).sum(dim=1).to(s["out"].dtype)
+    d = s["dout"].float()
+    dw = (picked * d.unsqueeze(1)).sum(dim=2)
+    here = (s["order"] >= 0).unsqueeze(1)
+    a = s["order"].clamp(min=0).long()
+    drows = torch.where(here, s["w"].reshape(-1)[a].unsqueeze(1) * d[a // k], 0.0)
+    return drows.to(s["drows"].dtype), dw
+
+
+def _plain_quantize(s):
+    case, x = s["case"], s["x"]
+    if case["of"] == "weights":
+        E, N, K = x.shape
+        q, scale = _eight_bits(torch.nn.functional.pad(x.float(), (0, _pad(K) - K, 0, _pad(N) - N)), True)
+        return q[:, :N].contiguous(), scale
+    x = x.float()
+    if case["of"] == "swiglu":
+        gate, up = x[:, : case["K"]], x[:, case["K"]:]
+        x = gate / (1.0 + torch.exp(-gate)) * up
+    return _quantized(x)
+
+
+def _plain_product(s):
+    N = s["w"].shape[1]
+    a = s["a"].float() * s["a_scale"].repeat_interleave(BLOCK, dim=1)
+    out = torch.zeros(s["out"].shape, device="cuda")
+    at = s["offsets"].tolist()
+    for e, (lo, hi) in enumerate(zip(at, at[1:])):
+        if hi > lo:
+            w = s["w"][e].float() * s["w_scale"][e].repeat_interleave(BLOCK, dim=0)[:N].repeat_interleave(BLOCK, dim=1)
+            out[lo:hi] = a[lo:hi] @ w.t()
+    return out.to(s["out"].dtype)
+
+
+# ---- the library's calls ----
+
+def _own_dispatch(s):
+    from paper_2603_09983_amd import binding as B
+    c = s["case"]
+    T, H, E, k = c["T"], c["H"], c["E"], c["k"]
+    if "workspace" not in s:
+        s["workspace"] = torch.empty(B.moe_sort_workspace_bytes(T, k, E), dtype=torch.uint8, device="cuda")
+    B.moe_sort_assignments(s["ids"], T, k, E, s["offsets"], s["order"], s["pos"], s["workspace"])
+    if c["fp8"]:
+        B.moe_permute_fp8(s["x"], c["bf16"], s["pos"], T, k, H, T * k, s["rows"], s["scale"])
+        return s["offsets"], s["order"], s["pos"], s["rows"], s["scale"]
+    B.moe_permute(s["x"], c["bf16"], s["pos"], T, k, H, T * k, s["rows"])
+    return s["offsets"], s["order"], s["pos"], s["rows"]
+
+
+def _own_combine(s):
+    from paper_2603_09983_amd import binding as B
+    c = s["case"]
+    T, H, k = c["T"], c["H"], c["k"]
+    if c["grad"]:
+        B.moe_unpermute_backward(s["dout"], c["out_bf16"], s["rows"], c["bf16"], s["pos"], s["w"], T, k, H, T * k, s["drows"], s["dw"])
+        return s["drows"], s["dw"]
+    B.moe_unpermute(s["rows"], c["bf16"], s["pos"], s["w"], T, k, H, T * k, s["out"], c["out_bf16"], False)
+    return s["out"]
+
+
+def _own_quantize(s):
+    from paper_2603_09983_amd import binding as B
+    c, x = s["case"], s["x"]
+    if c["of"] == "weights":
+        B.moe_quantize_weights_fp8(x, c["bf16"], c["E"], c["N"], c["K"], s["q"], s["scale"])
+    elif c["of"] == "swiglu":
+        B.moe_swiglu_fp8(x, c["bf16"], None, c["M"], c["K"], s["q"], s["scale"])
+    else:
+        B.moe_quantize_fp8(x, c["bf16"], None, c["M"], c["K"], s["q"], s["scale"])
+    return s["q"], s["scale"]
+
+
+def _own_product(s):
+    from paper_2603_09983_amd import binding as B
+    E, N, Kp = s["w"].shape
+    B.moe_grouped_matmul_fp8(s["a"], s["a_scale"], s["w"], s["w_scale"], s["offsets"], s["a"].shape[0], N, Kp, E, s["out"],
+                             s["case"]["out_bf16"])
+    return s["out"]
+
+
+def run(state):
+    op = state["case"]["op"]
+    if own:
+        return {"dispatch": _own_dispatch, "combine": _own_combine, "quantize": _own_quantize, "product": _own_product}[op](state)
+    return {"dispatch": _plain_dispatch, "combine": _plain_combine, "quantize": _plain_quantize, "product": _plain_product}[op](state)
+
+
+# ---- the definitions in 64 bits ----
+
+def _exact_eight_bits(x, h):
+    """q (not rounded) and scale of blocks of h x 128 of x [N,K] in 64 bits, N and K any."""
+    N, K = x.shape
+    whole = torch.zeros((-(-N // h) * h, _pad(K)), dtype=torch.float64, device=x.device)
+    whole[:N, :K] = x
+    tiles = whole.unfold(0, h, h).unfold(1, BLOCK, BLOCK)          # [N/h, Kb, h, 128]
+    m = tiles.abs().flatten(2).max(dim=2).values.clamp(min=LEAST)
+    wide = m.repeat_interleave(h, dim=0).repeat_interleave(BLOCK, dim=1)
+    return (whole / wide * TOP)[:N], m / TOP
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    op = case["op"]
+    if op == "dispatch":
+        ids = s["ids"].reshape(-1).tolist()
+        order = [a for _, a in sorted((e, a) for a, e in enumerate(ids) if e >= 0)]
+        token = torch.tensor(order, dtype=torch.int64, device="cuda") // case["k"]
+        x = s["x"].double()
+        rows = torch.zeros(s["rows"].shape, dtype=torch.float64, device="cuda")
+        if not case["fp8"]:
+            rows[: len(order)] = x[token]
+            return None, None, None, rows
+        q, scale = _exact_eight_bits(x, 1)
+        scales = torch.zeros(s["scale"].shape, dtype=torch.float64, device="cuda")
+        rows[: len(order)], scales[: len(order)] = q[token], scale[token]
+        return None, None, None, rows, scales
+    if op == "combine":
+        T, k, H = case["T"], case["k"], case["H"]
+        rows, w, pos = s["rows"].double(), s["w"].double(), s["pos"].long()
+        if not case["grad"]:
+            out = torch.zeros((T, H), dtype=torch.float64, device="cuda")
+            for j in range(k):
+                t = (pos[:, j] >= 0).nonzero().squeeze(1)
+                out[t] += w[t, j].unsqueeze(1) * rows[pos[t, j]]
+            return out
+        d = s["dout"].double()
+        drows, dw = torch.zeros_like(rows), torch.zeros_like(w)
+        for j in range(k):
+            t = (pos[:, j] >= 0).nonzero().squeeze(1)
+            drows[pos[t, j]] = w[t, j].unsqueeze(1) * d[t]
+            dw[t, j] = (rows[pos[t, j]] * d[t]).sum(dim=1)
+        return drows, dw
+    if op == "quantize":
+        if case["of"] == "weights":
+            got = [_exact_eight_bits(m.double(), BLOCK) for m in s["x"]]
+            return torch.stack([q for q, _ in got]), torch.stack([c for _, c in got])
+        x = s["x"].double()
+        if case["of"] == "swiglu":
+            x = x[:, : case["K"]] * torch.sigmoid(x[:, : case["K"]]) * x[:, case["K"]:]
+        return _exact_eight_bits(x, 1)
+    N, Kp = s["w"].shape[1:]
+    out = torch.zeros(s["out"].shape, dtype=torch.float64, device="cuda")
+    at = s["offsets"].tolist()
+    for e in range(case["E"]):
+        rows = slice(at[e], at[e + 1])
+        if at[e] == at[e + 1]:
+            continue
+        for b in range(Kp // BLOCK):
+            cols = slice(b * BLOCK, (b + 1) * BLOCK)
+            part = s["a"][rows, cols].double() @ s["w"][e, :, cols].double().t()
+            sw = s["w_scale"][e, :, b].double().repeat_interleave(BLOCK)[:N]
+            out[rows] += part * s["a_scale"][rows, b].double().unsqueeze(1) * sw
+    return out
