@@ -177,7 +177,7 @@ def _eight_bits(x, tall):
     h = BLOCK if tall else 1
     b = x.reshape(-1, n // h, h, kb, BLOCK)
     m = b.abs().amax(dim=(2, 4), keepdim=True).clamp(min=LEAST)
-    q = (b * (TOP / m)).to(F8).reshape(x.shape)
+    q = (b * (torch.full_like(m, TOP) / m)).to(F8).reshape(x.shape)   # (TOP / m would be m's reciprocal times TOP)
     return q, (m / TOP).reshape(*x.shape[:-2], n // h, kb)
 
 
