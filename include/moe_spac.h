@@ -23,7 +23,7 @@
  *     slots, A = T*k assignments (flat id a = t*k + j).
  *   - Return value: MOE_OK, or a negative code; on a negative code nothing
  *     was launched.  No exceptions, no abort, nothing printed.
- *   - Supported sizes: 1 <= k <= min(E, 64); E <= 512; T*E <= 65536;
+ *   - Supported sizes (of the layer and its steps): 1 <= k <= min(E, 64); E <= 512; T*E <= 65536;
  *     C <= 1024; H, F and F_shared multiples of 8 (rows of 16 bytes); bf16
  *     tensors and `out` 16-byte aligned.  Any H with H, F and F_shared
  *     multiples of 64 and up to 32 tokens; every other shape is limited to
@@ -73,7 +73,8 @@ enum {
     MOE_OK = 0,
     MOE_ERR_NULL = -1,      /* a required pointer is NULL                              */
     MOE_ERR_SHAPE = -2,     /* a size is out of the supported range                    */
-    MOE_ERR_ALIGN = -3,     /* H or F not a multiple of 8, or a misaligned pointer      */
+    MOE_ERR_ALIGN = -3,     /* a width that is not a multiple of 8 (or of what the call
+                               asks for), or a misaligned pointer                       */
     MOE_ERR_WORKSPACE = -4, /* workspace_bytes is smaller than the call needs          */
     MOE_ERR_LAUNCH = -5,    /* the HIP runtime refused a launch or an attribute        */
     MOE_ERR_SCRATCH = -6    /* moe_verify_layer_static: the shape needs more scratch memory
@@ -325,6 +326,90 @@ int moe_pool_load(const void *store_gate, const void *store_up, const void *stor
                   void *pool_up, void *pool_down, const int32_t *fetch_list, const int32_t *fetch_slot,
                   const int32_t *n_fetch, int max_fetch, int H, int F, void *stream);
 
+/* ROWS SORTED BY EXPERT, for batches of any length and for programs with
+ * expert products of their own.  None of the calls below uses the state of a
+ * workspace, waits for another workgroup or synchronises: calls on different
+ * streams may run at the same time (with a workspace each, where one is
+ * taken), and each can be captured into a graph.  T*k <= 2^30; sizes beyond
+ * the limits are MOE_ERR_SHAPE.  Pointers to rows are 16-byte aligned, widths
+ * multiples of 8 (MOE_ERR_ALIGN).  x_bf16, rows_bf16, out_bf16, w_bf16:
+ * elements are bf16 (non-zero) or fp32 (0). */
+
+/* Assignments sorted by expert (stable).  ids [T,k] int32: experts
+ * (topk_idx) or slots (slot_idx); values outside [0,E) are assignments of no
+ * row.  E <= 1024.  Outputs, all int32:
+ *   offsets [E+1]  expert e has the rows [offsets[e], offsets[e+1]);
+ *   order [T*k]    row r holds assignment order[r] (flat id t*k + j), ids
+ *                  ascending inside an expert; -1 from offsets[E] on;
+ *   pos [T,k]      the row of an assignment, or -1.
+ * workspace: moe_sort_workspace_bytes(T, k, E) bytes, 16-byte aligned, needs
+ * no initialisation and holds nothing between calls. */
+int moe_sort_workspace_bytes(int T, int k, int E, size_t *bytes_out);
+int moe_sort_assignments(const int32_t *ids, int T, int k, int E, int32_t *offsets, int32_t *order, int32_t *pos,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* Tokens' rows into sorted order: out[pos[t,j],:] = x[t,:].  x [T,H]; out
+ * [R,H] of the same type; pos [T,k]: distinct rows, or values outside [0,R)
+ * for assignments of no row.  Rows of `out` that pos does not name are left as
+ * they were.  Its gradient is moe_unpermute with topk_w = NULL. */
+int moe_permute(const void *x, int x_bf16, const int32_t *pos, int T, int k, int H, int R, void *out, void *stream);
+
+/* ... each row quantised on the way as by moe_quantize_fp8: q [R,Hp] e4m3,
+ * scale [R,Hp/128]. */
+int moe_permute_fp8(const void *x, int x_bf16, const int32_t *pos, int T, int k, int H, int R, void *q, float *scale,
+                    void *stream);
+
+/* Back into token order:  out[t,:] (+)= sum over j of topk_w[t,j] rows[pos[t,j],:],
+ * summed in fp32, j ascending; values of pos outside [0,R) add nothing.
+ * rows [R,H]; topk_w [T,k] fp32 or NULL (all ones); out [T,H]; accumulate != 0
+ * adds to what `out` holds (before the first j), else `out` is overwritten. */
+int moe_unpermute(const void *rows, int rows_bf16, const int32_t *pos, const float *topk_w, int T, int k, int H, int R,
+                  void *out, int out_bf16, int accumulate, void *stream);
+
+/* Its gradient:  drows[pos[t,j],:] = topk_w[t,j] dout[t,:] (rows that pos does
+ * not name are left as they were; pos names distinct rows),
+ * dtopk_w[t,j] = <dout[t,:], rows[pos[t,j],:]> in fp32 (0 where pos[t,j] is
+ * outside [0,R)).  dout [T,H]; drows [R,H] of the type of rows, or NULL;
+ * dtopk_w [T,k] fp32, or NULL; not both NULL.  rows may be NULL without
+ * dtopk_w. */
+int moe_unpermute_backward(const void *dout, int dout_bf16, const void *rows, int rows_bf16, const int32_t *pos,
+                           const float *topk_w, int T, int k, int H, int R, void *drows, float *dtopk_w, void *stream);
+
+/* EXPERTS IN 8 BITS.  Values in e4m3 with one fp32 scale for each block of
+ * 128: with m = the block's largest magnitude, 2^-100 at least,
+ *   scale = m / 448,   q = x * (448 / m) rounded to nearest, ties to even,
+ * x = scale * q.  A block with NaN gets the scale NaN, one with an infinity
+ * the scale infinity and NaN in the infinity's place.  A row of K values
+ * (K % 8 == 0) takes Kp = 128 * ceil(K/128) bytes, zero behind the K-th.
+ *
+ * Rows: x [M,K] -> q [M,Kp], scale [M,Kp/128], blocks of 128 of a row.
+ * n_rows: device pointer to the number of rows that hold something (offsets + E
+ * of a sort; clamped to [0,M]; later rows are left as they were), or NULL: M. */
+int moe_quantize_fp8(const void *x, int x_bf16, const int32_t *n_rows, int M, int K, void *q, float *scale, void *stream);
+
+/* ... of silu(gate) * up, computed in fp32: gate_up [M,2F] holds gate in the
+ * first F columns, up in the others; q [M,Fp], scale [M,Fp/128]. */
+int moe_swiglu_fp8(const void *gate_up, int x_bf16, const int32_t *n_rows, int M, int F, void *q, float *scale, void *stream);
+
+/* Weights: w [E,N,K] -> q [E,N,Kp], scale [E,ceil(N/128),Kp/128], blocks of
+ * 128 x 128 (fewer rows at the end of a matrix).  E <= 1024. */
+int moe_quantize_weights_fp8(const void *w, int w_bf16, int E, int N, int K, void *q, float *scale, void *stream);
+
+/* Products of sorted rows with their experts' weights:
+ *   out[r,n] = sum over blocks b of  x_scale[r,b] w_scale[e,n/128,b] *
+ *              sum over the 128 columns i of b of  x[r,i] w[e,n,i],
+ * for offsets[e] <= r < offsets[e+1], summed in fp32.  x [M,K], w [E,N,K]
+ * e4m3 with K a multiple of 128 (the padded width), N a multiple of 8 (else
+ * MOE_ERR_ALIGN); offsets [E+1] int32, not descending, values clamped to
+ * [0,M]; out [M,N].  Rows of no expert are left as they were.  fp32 results:
+ * sums in 32 bits throughout.  bf16 results: the 128 products of a block are
+ * added by the 8-bit matrix instruction, which cuts the smaller ones of each
+ * eight at 2^-13 of the largest (about 2e-5 of the results' norm).  E <= 1024;
+ * E = 1 with offsets {0, M} is the plain product.  The gradient to x is the
+ * same call on the quantised gradient and the transposed weights. */
+int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const void *w, const float *w_scale,
+                           const int32_t *offsets, int M, int N, int K, int E, void *out, int out_bf16, void *stream);
+
 /* Measurement aid (host-side state only; not part of the layer's arithmetic).
  * While enabled, every kernel the library launches is bracketed by a pair of
  * HIP events recorded on the caller's stream.  kind: MOE_KERNEL_*.
@@ -337,7 +422,8 @@ int moe_pool_load(const void *store_gate, const void *store_up, const void *stor
 enum { MOE_KERNEL_ROUTE = 0, MOE_KERNEL_LISTS = 1, MOE_KERNEL_FFN = 2 /* gate/up (and down when fused) */,
        MOE_KERNEL_COMBINE = 3, MOE_KERNEL_DOWN = 4, MOE_KERNEL_ESTIMATOR = 5, MOE_KERNEL_BALANCER = 6,
        MOE_KERNEL_CACHE_PLAN = 7, MOE_KERNEL_POOL_LOAD = 8, MOE_KERNEL_LAYER = 9 /* the one-launch layer kernel */,
-       MOE_KERNEL_KINDS = 10 };
+       MOE_KERNEL_SORT = 10, MOE_KERNEL_PERMUTE = 11, MOE_KERNEL_UNPERMUTE = 12, MOE_KERNEL_QUANTIZE = 13,
+       MOE_KERNEL_MATMUL = 14, MOE_KERNEL_KINDS = 15 };
 int moe_profile_enable(int on);
 int moe_profile_read(int kind, double *total_ms, int *launches);
 const char *moe_profile_kernel_name(int kind);

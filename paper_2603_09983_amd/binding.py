@@ -69,6 +69,22 @@ for _f in ("moe_utility_init", "moe_utility_update", "moe_workspace_bytes", "moe
            "moe_slot_resolve", "moe_grouped_ffn", "moe_verify_layer"):
     getattr(_lib, _f).restype = _i
 
+_lib.moe_sort_workspace_bytes.argtypes = [_i] * 3 + [ctypes.POINTER(_sz)]
+_lib.moe_sort_assignments.argtypes = [_vp] + [_i] * 3 + [_vp] * 4 + [_sz, _vp]
+_lib.moe_permute.argtypes = [_vp, _i, _vp] + [_i] * 4 + [_vp] * 2
+_lib.moe_permute_fp8.argtypes = [_vp, _i, _vp] + [_i] * 4 + [_vp] * 3
+_lib.moe_unpermute.argtypes = [_vp, _i, _vp, _vp] + [_i] * 4 + [_vp, _i, _i, _vp]
+_lib.moe_unpermute_backward.argtypes = [_vp, _i, _vp, _i, _vp, _vp] + [_i] * 4 + [_vp] * 3
+_lib.moe_quantize_fp8.argtypes = [_vp, _i, _vp, _i, _i] + [_vp] * 3
+_lib.moe_swiglu_fp8.argtypes = [_vp, _i, _vp, _i, _i] + [_vp] * 3
+_lib.moe_quantize_weights_fp8.argtypes = [_vp] + [_i] * 4 + [_vp] * 3
+_lib.moe_grouped_matmul_fp8.argtypes = [_vp] * 5 + [_i] * 4 + [_vp, _i, _vp]
+ROWS_EXPORTS = ("moe_sort_workspace_bytes", "moe_sort_assignments", "moe_permute", "moe_permute_fp8", "moe_unpermute",
+                "moe_unpermute_backward", "moe_quantize_fp8", "moe_swiglu_fp8", "moe_quantize_weights_fp8",
+                "moe_grouped_matmul_fp8")
+for _f in ROWS_EXPORTS:
+    getattr(_lib, _f).restype = _i
+
 _lib.moe_profile_enable.argtypes = [_i]
 _lib.moe_profile_enable.restype = _i
 _lib.moe_profile_read.argtypes = [_i, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i)]
@@ -79,10 +95,11 @@ _lib.moe_profile_stream_timeline.argtypes = [ctypes.c_void_p, _sz]
 _lib.moe_profile_stream_timeline.restype = _i
 _lib.moe_profile_kernel_name.argtypes = [_i]
 _lib.moe_profile_kernel_name.restype = ctypes.c_char_p
-KERNEL_ROUTE, KERNEL_LISTS, KERNEL_FFN, KERNEL_COMBINE, KERNEL_DOWN, KERNEL_ESTIMATOR, KERNEL_BALANCER, KERNEL_CACHE_PLAN, KERNEL_POOL_LOAD, KERNEL_LAYER, KERNEL_KINDS = 0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10
+KERNEL_ROUTE, KERNEL_LISTS, KERNEL_FFN, KERNEL_COMBINE, KERNEL_DOWN, KERNEL_ESTIMATOR, KERNEL_BALANCER, KERNEL_CACHE_PLAN, KERNEL_POOL_LOAD, KERNEL_LAYER = 0, 1, 2, 3, 4, 5, 6, 7, 8, 9
+KERNEL_SORT, KERNEL_PERMUTE, KERNEL_UNPERMUTE, KERNEL_QUANTIZE, KERNEL_MATMUL, KERNEL_KINDS = 10, 11, 12, 13, 14, 15
 
 EXPORTS = ("moe_profile_stream_timeline", "moe_cache_plan", "moe_pool_load", "moe_balance_threshold", "moe_utility_init", "moe_utility_update", "moe_profile_event_overhead", "moe_profile_enable", "moe_profile_read", "moe_profile_kernel_name", "moe_status_string", "moe_workspace_bytes", "moe_workspace_init", "moe_workspace_status", "moe_workspace_wait_test", "moe_route_topk",
-           "moe_expert_histogram", "moe_slot_resolve", "moe_grouped_ffn", "moe_verify_layer", "moe_verify_layer_static")
+           "moe_expert_histogram", "moe_slot_resolve", "moe_grouped_ffn", "moe_verify_layer", "moe_verify_layer_static") + ROWS_EXPORTS
 
 
 class MoeError(RuntimeError):
@@ -301,6 +318,63 @@ def moe_pool_load(store_gate, store_up, store_down, pool_gate, pool_up, pool_dow
                             *_pointers(pool_gate, pool_up, pool_down, fetch_list, fetch_slot, n_fetch), max_fetch, H, F,
                             _stream(stream))
     return _check(rc, "moe_pool_load", check)
+
+
+def moe_sort_workspace_bytes(T, k, E) -> int:
+    out = _sz(0)
+    _check(_lib.moe_sort_workspace_bytes(T, k, E, ctypes.byref(out)), "moe_sort_workspace_bytes", True)
+    return int(out.value)
+
+
+def moe_sort_assignments(ids, T, k, E, offsets, order, pos, workspace, stream=None, check=True) -> int:
+    p = _pointers(ids, offsets, order, pos, workspace)
+    rc = _lib.moe_sort_assignments(p[0], T, k, E, *p[1:], 0 if workspace is None else workspace.numel(), _stream(stream))
+    return _check(rc, "moe_sort_assignments", check)
+
+
+def moe_permute(x, x_bf16, pos, T, k, H, R, out, stream=None, check=True) -> int:
+    p = _pointers(x, pos, out)
+    return _check(_lib.moe_permute(p[0], int(x_bf16), p[1], T, k, H, R, p[2], _stream(stream)), "moe_permute", check)
+
+
+def moe_permute_fp8(x, x_bf16, pos, T, k, H, R, q, scale, stream=None, check=True) -> int:
+    p = _pointers(x, pos, q, scale)
+    return _check(_lib.moe_permute_fp8(p[0], int(x_bf16), p[1], T, k, H, R, *p[2:], _stream(stream)), "moe_permute_fp8", check)
+
+
+def moe_unpermute(rows, rows_bf16, pos, topk_w, T, k, H, R, out, out_bf16, accumulate, stream=None, check=True) -> int:
+    p = _pointers(rows, pos, topk_w, out)
+    rc = _lib.moe_unpermute(p[0], int(rows_bf16), p[1], p[2], T, k, H, R, p[3], int(out_bf16), int(accumulate), _stream(stream))
+    return _check(rc, "moe_unpermute", check)
+
+
+def moe_unpermute_backward(dout, dout_bf16, rows, rows_bf16, pos, topk_w, T, k, H, R, drows, dtopk_w, stream=None,
+                           check=True) -> int:
+    p = _pointers(dout, rows, pos, topk_w, drows, dtopk_w)
+    rc = _lib.moe_unpermute_backward(p[0], int(dout_bf16), p[1], int(rows_bf16), p[2], p[3], T, k, H, R, *p[4:], _stream(stream))
+    return _check(rc, "moe_unpermute_backward", check)
+
+
+def moe_quantize_fp8(x, x_bf16, n_rows, M, K, q, scale, stream=None, check=True) -> int:
+    p = _pointers(x, n_rows, q, scale)
+    return _check(_lib.moe_quantize_fp8(p[0], int(x_bf16), p[1], M, K, *p[2:], _stream(stream)), "moe_quantize_fp8", check)
+
+
+def moe_swiglu_fp8(gate_up, x_bf16, n_rows, M, F, q, scale, stream=None, check=True) -> int:
+    p = _pointers(gate_up, n_rows, q, scale)
+    return _check(_lib.moe_swiglu_fp8(p[0], int(x_bf16), p[1], M, F, *p[2:], _stream(stream)), "moe_swiglu_fp8", check)
+
+
+def moe_quantize_weights_fp8(w, w_bf16, E, N, K, q, scale, stream=None, check=True) -> int:
+    p = _pointers(w, q, scale)
+    return _check(_lib.moe_quantize_weights_fp8(p[0], int(w_bf16), E, N, K, *p[1:], _stream(stream)), "moe_quantize_weights_fp8",
+                  check)
+
+
+def moe_grouped_matmul_fp8(x, x_scale, w, w_scale, offsets, M, N, K, E, out, out_bf16, stream=None, check=True) -> int:
+    p = _pointers(x, x_scale, w, w_scale, offsets, out)
+    rc = _lib.moe_grouped_matmul_fp8(*p[:5], M, N, K, E, p[5], int(out_bf16), _stream(stream))
+    return _check(rc, "moe_grouped_matmul_fp8", check)
 
 
 # ---------------------------------------------------------------------------

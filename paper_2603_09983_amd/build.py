@@ -21,8 +21,9 @@ LIB = os.path.join(HERE, "libmoe_spac.so")
 LIB_POINTERS = os.path.join(HERE, "_pointers" + sysconfig.get_config_var("EXT_SUFFIX"))
 POINTERS_STAMP = os.path.join(OBJ_DIR, "pointers.stamp")
 LIB_TRACE = os.path.join(HERE, "libmoe_spac_trace.so")   # same sources with the timeline stamps compiled in
-SOURCES = ["api.hip", "route.hip", "ffn.hip", "stream.hip", "wide.hip", "layer.hip", "estimator.hip", "balancer.hip", "cache.hip"]
-HEADERS = [os.path.join(CSRC, h) for h in ("moe_internal.h", "route_device.h", "wide_device.h")] + \
+SOURCES = ["api.hip", "route.hip", "ffn.hip", "stream.hip", "wide.hip", "layer.hip", "estimator.hip", "balancer.hip", "cache.hip",
+           "permute.hip", "fp8.hip", "fp8_matmul.hip"]
+HEADERS = [os.path.join(CSRC, h) for h in ("moe_internal.h", "route_device.h", "wide_device.h", "rows_device.h")] + \
           [os.path.join(ROOT, "include", "moe_spac.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed-fp32 instruction selection is switched off for every kernel of this library

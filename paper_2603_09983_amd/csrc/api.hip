@@ -11,12 +11,6 @@ namespace {
 
 thread_local char g_launch_msg[160] = "HIP launch error";
 
-int launch_failed(hipError_t e)
-{
-    snprintf(g_launch_msg, sizeof g_launch_msg, "HIP launch error: %s", hipGetErrorString(e));
-    return MOE_ERR_LAUNCH;
-}
-
 // ---- measurement aid: event pairs around each launch ----
 constexpr int kProfMax = 8192;
 struct ProfState {
@@ -25,8 +19,6 @@ struct ProfState {
     int created[MOE_KERNEL_KINDS] = {};   // pairs made so far, per kind
     int used[MOE_KERNEL_KINDS] = {};
 } g_prof;
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int check_route_shape(int T, int H, int E, int k)
 {
@@ -93,6 +85,21 @@ hipError_t moe::allow_full_lds(const void *fn, int bytes)
     e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e == hipSuccess) d.lds_allowed[fn] = bytes;
     return e;
+}
+
+int moe::launch_failed(hipError_t e)
+{
+    snprintf(g_launch_msg, sizeof g_launch_msg, "HIP launch error: %s", hipGetErrorString(e));
+    return MOE_ERR_LAUNCH;
+}
+
+int moe::launch_rows(const void *fn, dim3 grid, int threads, void *args, size_t lds, void *stream, int kind)
+{
+    void *params[] = {args};
+    hipError_t e = lds > 65536 ? allow_full_lds(fn) : hipSuccess;
+    if (e == hipSuccess) e = launch_timed(fn, grid, dim3(threads), params, lds, (hipStream_t)stream, kind);
+    if (e == hipSuccess) e = hipGetLastError();
+    return e == hipSuccess ? MOE_OK : launch_failed(e);
 }
 
 // One kernel launch, bracketed by a pair of events on its stream while the measurement aid is on.
@@ -203,6 +210,11 @@ extern "C" const char *moe_profile_kernel_name(int kind)
     case MOE_KERNEL_CACHE_PLAN: return "plan_kernel";
     case MOE_KERNEL_POOL_LOAD: return "load_kernel";
     case MOE_KERNEL_LAYER: return "layer_kernel";
+    case MOE_KERNEL_SORT: return "sort_kernels";
+    case MOE_KERNEL_PERMUTE: return "permute_kernels";
+    case MOE_KERNEL_UNPERMUTE: return "unpermute_kernels";
+    case MOE_KERNEL_QUANTIZE: return "quantize_kernels";
+    case MOE_KERNEL_MATMUL: return "grouped_matmul_kernels";
     default: return "?";
     }
 }
@@ -213,7 +225,7 @@ extern "C" const char *moe_status_string(int status)
     case MOE_OK: return "ok";
     case MOE_ERR_NULL: return "a required pointer is NULL";
     case MOE_ERR_SHAPE: return "a size is outside the supported range";
-    case MOE_ERR_ALIGN: return "H or F is not a multiple of 8, or a pointer is not 16-byte aligned";
+    case MOE_ERR_ALIGN: return "a width is not a multiple of 8 (of 128: columns of a product in 8 bits), or a pointer is not 16-byte aligned";
     case MOE_ERR_WORKSPACE: return "workspace is smaller than moe_workspace_bytes() asks for, or has served another shape since moe_workspace_init";
     case MOE_ERR_LAUNCH: return g_launch_msg;
     case MOE_ERR_SCRATCH: return "the shape needs more scratch memory than the library's static array holds";
