@@ -22,7 +22,7 @@ struct MatmulArgs {
     const float *a_scale, *w_scale;   // [M,K/128], [E,ceil(N/128),K/128]
     const int32_t *offsets;      // [E+1]
     void *out;                   // [M,N]
-    int M, N, K;
+    int M, N, K, E;
 };
 
 // 128 columns' products of sixteen weight rows and sixteen tokens (each lane: 32 columns of one row of both).
@@ -132,6 +132,213 @@ __global__ __launch_bounds__(kThreads) void grouped_matmul_kernel(MatmulArgs a)
     }
 }
 
+// ---- many rows to an expert: tiles of 256 weight rows x 256 tokens through LDS ----
+// Bound by the matrix cores.  One workgroup of eight wavefronts per CU walks the tiles; a step is one block of 128 columns: 32 KB of
+// weights and 32 KB of rows, which the next step's loads bring into the other half of LDS while this one multiplies.  A wavefront has
+// 128 weight rows x 64 tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core) four multiply-adds (16 cycles of the vector
+// ALU) bring the block's sum, times its scales, into the tile's.
+//
+// LDS: a row's eight 16-byte words are permuted by a key of the row, so that the eight lanes that a read serves at a time find eight
+// different words.  Weight rows go to the matrix rows so that a lane's results of two products are eight consecutive columns of `out`.
+constexpr int kTile = 256, kTileThreads = 512;
+constexpr int kTileBytes = kTile * kBlock, kStageBytes = 2 * kTileBytes;
+constexpr int kTileScales = 2 * kStageBytes, kTileTable = kTileScales + 2 * kTile * 4;
+constexpr int kTileLds = kTileTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
+static_assert(kTileLds <= kLdsBytes, "two stages, their scales, the experts' first tiles");
+
+// 16 (or 4) bytes a lane from base + at to LDS, lane after lane from `to` on.  Not waited for by the compiler: the loop counts.
+__device__ __forceinline__ void fetch16(uint32_t to, uint32_t at, const void *base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
+}
+__device__ __forceinline__ void fetch4(uint32_t to, uint32_t at, const void *base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
+}
+
+__device__ __forceinline__ int clamped(int v, int most) { return v < 0 ? 0 : v > most ? most : v; }
+
+// first[e] = tiles of 256 rows of the experts before e, e = 0..E (all threads of a workgroup; E <= 2 * threads).  No more than there
+// can be where no expert's rows are another's too.
+__device__ __forceinline__ void count_tiles(const int32_t *offsets, int M, int E, int32_t *first, int32_t *wave_sum)
+{
+    const int most = (M + kTile - 1) / kTile + (E < M ? E : M);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
+    int n[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int e = 2 * tid + i;
+        n[i] = 0;
+        if (e < E) {
+            const int rows = clamped(offsets[e + 1], M) - clamped(offsets[e], M);
+            n[i] = rows > 0 ? (rows + kTile - 1) / kTile : 0;
+        }
+    }
+    int up = n[0] + n[1];
+    for (int d = 1; d < kWave; d <<= 1) {
+        const int o = __shfl_up(up, d);
+        if (lane >= d) up += o;
+    }
+    if (lane == kWave - 1) wave_sum[w] = up;
+    __syncthreads();
+    int before = up - n[0] - n[1];
+    for (int v = 0; v < w; ++v) before += wave_sum[v];
+    auto put = [&](int e, int v) {
+        if (e <= E) first[e] = v < most ? v : most;
+    };
+    put(2 * tid, before);
+    put(2 * tid + 1, before + n[0]);
+    if (tid == kTileThreads - 1) put(2 * kTileThreads, before + n[0] + n[1]);
+    __syncthreads();
+}
+
+template <bool OUT16>
+__global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    int32_t *first = (int32_t *)(lds + kTileTable);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock, tiles_n = (a.N + kTile - 1) / kTile, nb = (a.N + kBlock - 1) / kBlock;
+    count_tiles(a.offsets, a.M, a.E, first, first + kMaxC + 1);
+    const int total = __builtin_amdgcn_readfirstlane(first[a.E]) * tiles_n;
+
+    // Where a tile lies.  An expert's tiles: its row tiles first, then the next 256 weight rows.
+    struct Place {
+        int e, n0, r0, end;
+    };
+    auto place = [&](int t) {
+        int e = -1;   // the last expert whose first tile is not behind t
+        for (int i = 0; i < a.E; i += kWave)
+            e += __popcll(__ballot(i + lane < a.E && first[i + lane < a.E ? i + lane : 0] * tiles_n <= t));
+        const int f = __builtin_amdgcn_readfirstlane(first[e]), m = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
+        const int local = t - f * tiles_n, n = local / m;
+        const int lo = clamped(a.offsets[e], a.M), hi = clamped(a.offsets[e + 1], a.M);
+        return Place{e, n * kTile, lo + (local - n * m) * kTile, hi};
+    };
+
+    // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word; tokens' scales.
+    const int frow = tid / 8, wkey = (frow & 3) | ((frow >> 1) & 4), xkey = frow & 7;
+    const uint8_t *wbase, *xbase;
+    const float *sbase;
+    uint32_t wat[4], xat[4], sat;
+    const float *swp;       // this wavefront's block row of the weights' scales
+    auto start = [&](const Place &p) {
+        wbase = a.w + ((size_t)p.e * a.N + p.n0) * a.K;
+        xbase = a.a + (size_t)p.r0 * a.K;
+        sbase = a.a_scale + (size_t)p.r0 * kb;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = frow + 64 * i < a.N - p.n0 ? frow + 64 * i : a.N - p.n0 - 1;
+            const int r = frow + 64 * i < p.end - p.r0 ? frow + 64 * i : p.end - p.r0 - 1;
+            wat[i] = (uint32_t)n * a.K + ((tid & 7) ^ wkey) * 16;
+            xat[i] = (uint32_t)r * a.K + ((tid & 7) ^ xkey) * 16;
+        }
+        const int r = (tid & (kTile - 1)) < p.end - p.r0 ? tid & (kTile - 1) : p.end - p.r0 - 1;
+        sat = (uint32_t)r * kb * 4;
+    };
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    auto fetch = [&](int stage) {
+        const uint32_t to = lds0 + stage * kStageBytes + w * 1024;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            fetch16(to + i * 8192, wat[i], wbase);
+            fetch16(to + kTileBytes + i * 8192, xat[i], xbase);
+        }
+        if (w < 4) fetch4(lds0 + kTileScales + stage * kTile * 4 + w * 256, sat, sbase);
+        wbase += kBlock;
+        xbase += kBlock;
+        ++sbase;
+    };
+
+    // Tiles b, b + G, .. of an order in which the workgroups of one XCD (b % 8) are neighbours.
+    const int G = gridDim.x, xcds = G % 8 ? 1 : 8, b0 = (blockIdx.x % xcds) * (G / xcds) + blockIdx.x / xcds;
+    const int wn = w & 1, wm = w >> 1;
+    const uint32_t wread = (128 * wn + 8 * (col >> 2) + (col & 3)) * kBlock + ((grp ^ (col & 7)) << 4);   // (the key of that row: col & 7)
+    const uint32_t xread = (64 * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
+    int stage = 0;
+    if (b0 >= total) return;
+    Place p = place(b0);
+    start(p);
+    fetch(0);
+    for (int t = b0; t < total; t += G) {
+        const Place here = p;
+        swp = a.w_scale + ((size_t)here.e * nb + (here.n0 / kBlock + wn < nb ? here.n0 / kBlock + wn : nb - 1)) * kb;
+        const bool mine = here.r0 + 64 * wm < here.end && here.n0 + 128 * wn < a.N;
+        f32x4 acc[8][4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int b = 0; b < kb; ++b) {
+            // this wavefront's part of the step has arrived and its reads of the step before are done; then everybody's
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (b + 1 < kb) {
+                fetch(stage ^ 1);
+            } else if (t + G < total) {
+                p = place(t + G);
+                start(p);
+                fetch(stage ^ 1);
+            }
+            if (mine) {
+                const uint8_t *wt = lds + stage * kStageBytes, *xt = wt + kTileBytes;
+                const float *st = (const float *)(lds + kTileScales + stage * kTile * 4) + 64 * wm + col;
+                const float sw = swp[b];
+                float s[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] = st[16 * j] * sw;
+                // (fp32 results: the wider operands of two token groups at a time, so that all stays in registers)
+                constexpr int J = OUT16 ? 4 : 2;
+#pragma unroll
+                for (int j0 = 0; j0 < 4; j0 += J) {
+                    if (J < 4) {   // (read and convert again: nothing of the first pass is kept for the second)
+                        asm volatile("" ::: "memory");
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    auto x = [&](int j) {
+                        const uint8_t *q = xt + (j0 + j) * 16 * kBlock;
+                        return Operand<!OUT16>(*(const u32x4 *)(q + xread), *(const u32x4 *)(q + (xread ^ 64)));
+                    };
+                    const Operand<!OUT16> xs[4] = {x(0), x(1), x(J == 4 ? 2 : 0), x(J == 4 ? 3 : 1)};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint8_t *q = wt + ((i >> 1) * 32 + (i & 1) * 4) * kBlock;
+                        const Operand<!OUT16> y(*(const u32x4 *)(q + wread), *(const u32x4 *)(q + (wread ^ 64)));
+                        f32x4 sum[J];
+#pragma unroll
+                        for (int j = 0; j < J; ++j) sum[j] = mfma128(y, xs[j]);
+#pragma unroll
+                        for (int j = 0; j < J; ++j)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) acc[i][j0 + j][c] = __builtin_fmaf(sum[j][c], s[j0 + j], acc[i][j0 + j][c]);
+                    }
+                }
+            }
+            stage ^= 1;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = here.r0 + 64 * wm + 16 * j + col;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int n = here.n0 + 128 * wn + 32 * i + 8 * grp;
+                if (r < here.end && n < a.N) {
+                    const f32x4 u = acc[2 * i][j], v = acc[2 * i + 1][j];
+                    if (OUT16) {
+                        const u32x4 o = {pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                        *(u32x4 *)((uint16_t *)a.out + (size_t)r * a.N + n) = o;
+                    } else {
+                        f32x4 *o = (f32x4 *)((float *)a.out + (size_t)r * a.N + n);
+                        o[0] = u;
+                        o[1] = v;
+                    }
+                }
+            }
+        }
+    }
+}
+
 }  // namespace
 
 }  // namespace moe
@@ -142,9 +349,18 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
                                       int M, int N, int K, int E, void *out, int out_bf16, void *stream)
 {
     if (!x || !x_scale || !w || !w_scale || !offsets || !out) return MOE_ERR_NULL;
-    if (M < 1 || N < 1 || K < 1 || E < 1 || E > kMaxC || M > 1 << 30 || N > 1 << 24 || K > 1 << 24) return MOE_ERR_SHAPE;
+    if (M < 1 || N < 1 || K < 1 || E < 1 || E > kMaxC || M > 1 << 30 || N > 1 << 24 || K > 1 << 20) return MOE_ERR_SHAPE;
     if (N % 8 || K % kBlock || !aligned16(x) || !aligned16(w) || !aligned16(out)) return MOE_ERR_ALIGN;
-    MatmulArgs a = {(const uint8_t *)x, (const uint8_t *)w, x_scale, w_scale, offsets, out, M, N, K};
+    MatmulArgs a = {(const uint8_t *)x, (const uint8_t *)w, x_scale, w_scale, offsets, out, M, N, K, E};
+    if (M / E >= 64) {
+        hipError_t err;
+        const int cus = device_cus(&err);
+        if (err != hipSuccess) return launch_failed(err);
+        const size_t most = ((size_t)(M + kTile - 1) / kTile + (E < M ? E : M)) * ((N + kTile - 1) / kTile);
+        if (most >= (size_t)1 << 30) return MOE_ERR_SHAPE;
+        return launch_rows(out_bf16 ? (const void *)tile_matmul_kernel<true> : (const void *)tile_matmul_kernel<false>,
+                           dim3(most < (size_t)cus ? (unsigned)most : cus), kTileThreads, &a, kTileLds, stream, MOE_KERNEL_MATMUL);
+    }
     return launch_rows(out_bf16 ? (const void *)grouped_matmul_kernel<true> : (const void *)grouped_matmul_kernel<false>,
                        dim3((N + 31) / 32, E), kThreads, &a, 0, stream, MOE_KERNEL_MATMUL);
 }
