@@ -142,7 +142,8 @@ __global__ __launch_bounds__(kThreads) void grouped_matmul_kernel(MatmulArgs a)
 // different words.  Weight rows go to the matrix rows so that a lane's results of two products are eight consecutive columns of `out`.
 constexpr int kTile = 256, kTileThreads = 512;
 constexpr int kTileBytes = kTile * kBlock, kStageBytes = 2 * kTileBytes;
-constexpr int kTileScales = 2 * kStageBytes, kTileTable = kTileScales + 2 * kTile * 4;
+constexpr int kStageScales = (kTile + kWave) * 4;   // of 256 tokens, of the two blocks of weight rows
+constexpr int kTileScales = 2 * kStageBytes, kTileTable = kTileScales + 2 * kStageScales;
 constexpr int kTileLds = kTileTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
 static_assert(kTileLds <= kLdsBytes, "two stages, their scales, the experts' first tiles");
 
@@ -216,16 +217,15 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
         return Place{e, n * kTile, lo + (local - n * m) * kTile, hi};
     };
 
-    // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word; tokens' scales.
+    // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word; a token's scale (wavefronts 0 to 3), or
+    // a weight row block's (wavefront 4).
     const int frow = tid / 8, wkey = (frow & 3) | ((frow >> 1) & 4), xkey = frow & 7;
     const uint8_t *wbase, *xbase;
     const float *sbase;
     uint32_t wat[4], xat[4], sat;
-    const float *swp;       // this wavefront's block row of the weights' scales
     auto start = [&](const Place &p) {
         wbase = a.w + ((size_t)p.e * a.N + p.n0) * a.K;
         xbase = a.a + (size_t)p.r0 * a.K;
-        sbase = a.a_scale + (size_t)p.r0 * kb;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int n = frow + 64 * i < a.N - p.n0 ? frow + 64 * i : a.N - p.n0 - 1;
@@ -233,8 +233,14 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
             wat[i] = (uint32_t)n * a.K + ((tid & 7) ^ wkey) * 16;
             xat[i] = (uint32_t)r * a.K + ((tid & 7) ^ xkey) * 16;
         }
-        const int r = (tid & (kTile - 1)) < p.end - p.r0 ? tid & (kTile - 1) : p.end - p.r0 - 1;
-        sat = (uint32_t)r * kb * 4;
+        if (w < 4) {
+            sbase = a.a_scale + (size_t)p.r0 * kb;
+            sat = (uint32_t)(tid < p.end - p.r0 ? tid : p.end - p.r0 - 1) * kb * 4;
+        } else {
+            const int n = p.n0 / kBlock;
+            sbase = a.w_scale + ((size_t)p.e * nb + n) * kb;
+            sat = (uint32_t)((lane & 1) < nb - n ? lane & 1 : 0) * kb * 4;
+        }
     };
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     auto fetch = [&](int stage) {
@@ -244,7 +250,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
             fetch16(to + i * 8192, wat[i], wbase);
             fetch16(to + kTileBytes + i * 8192, xat[i], xbase);
         }
-        if (w < 4) fetch4(lds0 + kTileScales + stage * kTile * 4 + w * 256, sat, sbase);
+        if (w < 5) fetch4(lds0 + kTileScales + stage * kStageScales + w * 256, sat, sbase);
         wbase += kBlock;
         xbase += kBlock;
         ++sbase;
@@ -262,7 +268,6 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     fetch(0);
     for (int t = b0; t < total; t += G) {
         const Place here = p;
-        swp = a.w_scale + ((size_t)here.e * nb + (here.n0 / kBlock + wn < nb ? here.n0 / kBlock + wn : nb - 1)) * kb;
         const bool mine = here.r0 + 64 * wm < here.end && here.n0 + 128 * wn < a.N;
         f32x4 acc[8][4];
 #pragma unroll
@@ -283,11 +288,10 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
             }
             if (mine) {
                 const uint8_t *wt = lds + stage * kStageBytes, *xt = wt + kTileBytes;
-                const float *st = (const float *)(lds + kTileScales + stage * kTile * 4) + 64 * wm + col;
-                const float sw = swp[b];
+                const float *st = (const float *)(lds + kTileScales + stage * kStageScales);
                 float s[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] = st[16 * j] * sw;
+                for (int j = 0; j < 4; ++j) s[j] = st[64 * wm + col + 16 * j] * st[kTile + wn];
                 // (fp32 results: the wider operands of two token groups at a time, so that all stays in registers)
                 constexpr int J = OUT16 ? 4 : 2;
 #pragma unroll
@@ -301,17 +305,28 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
                         return Operand<!OUT16>(*(const u32x4 *)(q + xread), *(const u32x4 *)(q + (xread ^ 64)));
                     };
                     const Operand<!OUT16> xs[4] = {x(0), x(1), x(J == 4 ? 2 : 0), x(J == 4 ? 3 : 1)};
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    auto y = [&](int i) {
                         const uint8_t *q = wt + ((i >> 1) * 32 + (i & 1) * 4) * kBlock;
-                        const Operand<!OUT16> y(*(const u32x4 *)(q + wread), *(const u32x4 *)(q + (wread ^ 64)));
-                        f32x4 sum[J];
+                        return Operand<!OUT16>(*(const u32x4 *)(q + wread), *(const u32x4 *)(q + (wread ^ 64)));
+                    };
+                    // a weight operand's products while the ones before are scaled and added (in this order: left to itself the
+                    // compiler puts every product's multiply-adds right behind it and waits)
+                    f32x4 sum[2][J];
+                    Operand<!OUT16> ys = y(0);
 #pragma unroll
-                        for (int j = 0; j < J; ++j) sum[j] = mfma128(y, xs[j]);
+                    for (int i = 0; i <= 8; ++i) {
+                        const Operand<!OUT16> now = ys;
+                        if (i < 7) ys = y(i + 1);
 #pragma unroll
-                        for (int j = 0; j < J; ++j)
+                        for (int j = 0; j < J; ++j) {
+                            if (i < 8) sum[i & 1][j] = mfma128(now, xs[j]);
+                            if (i > 0) {
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) acc[i][j0 + j][c] = __builtin_fmaf(sum[j][c], s[j0 + j], acc[i][j0 + j][c]);
+                                for (int c = 0; c < 4; ++c)
+                                    acc[i - 1][j0 + j][c] = __builtin_fmaf(sum[~i & 1][j][c], s[j0 + j], acc[i - 1][j0 + j][c]);
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
                     }
                 }
             }
