@@ -23,6 +23,7 @@ struct MatmulArgs {
     const int32_t *offsets;      // [E+1]
     void *out;                   // [M,N]
     int M, N, K, E;
+    int scale_words;             // the rows' scales are whole 16-byte words
 };
 
 // 128 columns' products of sixteen weight rows and sixteen tokens (each lane: 32 columns of one row of both).
@@ -47,6 +48,7 @@ struct Operand;
 template <>
 struct Operand<false> {
     i32x8 v;
+    Operand() = default;
     __device__ __forceinline__ Operand(u32x4 a, u32x4 b)
         : v{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]}
     {
@@ -55,6 +57,7 @@ struct Operand<false> {
 template <>
 struct Operand<true> {
     bf16x8 v[4];
+    Operand() = default;
     __device__ __forceinline__ Operand(u32x4 a, u32x4 b)
         : v{widen8(a[0], a[1]), widen8(a[2], a[3]), widen8(b[0], b[1]), widen8(b[2], b[3])}
     {
@@ -133,17 +136,22 @@ __global__ __launch_bounds__(kThreads) void grouped_matmul_kernel(MatmulArgs a)
 }
 
 // ---- many rows to an expert: tiles of 256 weight rows x 256 tokens through LDS ----
-// Bound by the matrix cores.  One workgroup of eight wavefronts per CU walks the tiles; a step is one block of 128 columns: 32 KB of
-// weights and 32 KB of rows, which the next step's loads bring into the other half of LDS while this one multiplies.  A wavefront has
-// 128 weight rows x 64 tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core) four multiply-adds (16 cycles of the vector
-// ALU) bring the block's sum, times its scales, into the tile's.
+// Bound by the matrix cores.  One workgroup of eight wavefronts per CU walks the tiles; a step is one block of 128 columns, 32 KB of
+// weights and 32 KB of rows.  A wavefront has 64 weight rows x 128 tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core)
+// four multiply-adds (16 cycles of the vector ALU) bring the block's sum, times its scales, into the tile's.
 //
-// LDS: a row's eight 16-byte words are permuted by a key of the row, so that the eight lanes that a read serves at a time find eight
+// LDS holds two steps.  A wavefront reads its weights of a step at its beginning and keeps them; once all have (a second barrier), the
+// weights of the step after next are requested into their place.  The rows of the next step are requested when everybody is through
+// with the step before.  So the weights, most of which come from HBM, have two steps' time to arrive, the rows, which other workgroups
+// of the XCD have mostly brought into its L2, one.
+//
+// A row's eight 16-byte words are permuted by a key of the row, so that the eight lanes that a read serves at a time find eight
 // different words.  Weight rows go to the matrix rows so that a lane's results of two products are eight consecutive columns of `out`.
 constexpr int kTile = 256, kTileThreads = 512;
 constexpr int kTileBytes = kTile * kBlock, kStageBytes = 2 * kTileBytes;
-constexpr int kStageScales = (kTile + kWave) * 4;   // of 256 tokens, of the two blocks of weight rows
-constexpr int kTileScales = 2 * kStageBytes, kTileTable = kTileScales + 2 * kStageScales;
+constexpr int kChunk = 4;                                  // blocks whose scales are fetched together
+constexpr int kChunkBytes = kChunk * (kTile + kWave) * 4;  // of 256 tokens, then of the two blocks of weight rows (and padding)
+constexpr int kTileScales = 2 * kStageBytes, kTileTable = kTileScales + 2 * kChunkBytes;
 constexpr int kTileLds = kTileTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
 static_assert(kTileLds <= kLdsBytes, "two stages, their scales, the experts' first tiles");
 
@@ -217,20 +225,33 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
         return Place{e, n * kTile, lo + (local - n * m) * kTile, hi};
     };
 
-    // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word; a token's scale (wavefronts 0 to 3), or
-    // a weight row block's (wavefront 4).
+    // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word each.
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     const int frow = tid / 8, wkey = (frow & 3) | ((frow >> 1) & 4), xkey = frow & 7;
     const uint8_t *wbase, *xbase;
-    const float *sbase;
-    uint32_t wat[4], xat[4], sat;
-    auto start = [&](const Place &p) {
+    uint32_t wat[4], xat[4];
+    auto start_w = [&](const Place &p) {
         wbase = a.w + ((size_t)p.e * a.N + p.n0) * a.K;
-        xbase = a.a + (size_t)p.r0 * a.K;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int n = frow + 64 * i < a.N - p.n0 ? frow + 64 * i : a.N - p.n0 - 1;
-            const int r = frow + 64 * i < p.end - p.r0 ? frow + 64 * i : p.end - p.r0 - 1;
             wat[i] = (uint32_t)n * a.K + ((tid & 7) ^ wkey) * 16;
+        }
+    };
+    auto fetch_w = [&](int stage, int i) {   // a quarter of a step's weights
+        fetch16(lds0 + stage * kStageBytes + w * 1024 + i * 8192, wat[i], wbase);
+        if (i == 3) wbase += kBlock;
+    };
+    // The rows, and the scales of four blocks at a time: tokens' by wavefronts 0 to 3, the weights' two block rows' by wavefront 4.
+    // In LDS [token][block] where a row's scales are whole 16-byte words, else [block][token].
+    const int by_word = a.scale_words, s_row = by_word ? kChunk * 4 : 4, s_block = by_word ? 4 : kTile * 4, sw_block = by_word ? 4 : kWave * 4;
+    const float *sbase;
+    uint32_t sat;
+    auto start_x = [&](const Place &p) {
+        xbase = a.a + (size_t)p.r0 * a.K;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = frow + 64 * i < p.end - p.r0 ? frow + 64 * i : p.end - p.r0 - 1;
             xat[i] = (uint32_t)r * a.K + ((tid & 7) ^ xkey) * 16;
         }
         if (w < 4) {
@@ -242,102 +263,140 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
             sat = (uint32_t)((lane & 1) < nb - n ? lane & 1 : 0) * kb * 4;
         }
     };
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-    auto fetch = [&](int stage) {
-        const uint32_t to = lds0 + stage * kStageBytes + w * 1024;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            fetch16(to + i * 8192, wat[i], wbase);
-            fetch16(to + kTileBytes + i * 8192, xat[i], xbase);
+    auto fetch_x = [&](int stage, int i) {
+        fetch16(lds0 + stage * kStageBytes + kTileBytes + w * 1024 + i * 8192, xat[i], xbase);
+        if (i == 3) xbase += kBlock;
+    };
+    int chunk = 1;   // which half of the scales' place holds the chunk fetched last
+    auto fetch_scales = [&](int b) {   // of blocks b .. b + 3
+        chunk ^= 1;
+        if (w >= 5) return;
+        const uint32_t to = lds0 + kTileScales + chunk * kChunkBytes + (w < 4 ? w * kWave * s_row : kChunk * kTile * 4);
+        if (by_word) {
+            fetch16(to, sat, sbase + b);
+        } else {
+            for (int i = 0; i < kChunk && b + i < kb; ++i) fetch4(to + i * (w < 4 ? s_block : sw_block), sat, sbase + b + i);
         }
-        if (w < 5) fetch4(lds0 + kTileScales + stage * kStageScales + w * 256, sat, sbase);
-        wbase += kBlock;
-        xbase += kBlock;
-        ++sbase;
     };
 
     // Tiles b, b + G, .. of an order in which the workgroups of one XCD (b % 8) are neighbours.
     const int G = gridDim.x, xcds = G % 8 ? 1 : 8, b0 = (blockIdx.x % xcds) * (G / xcds) + blockIdx.x / xcds;
-    const int wn = w & 1, wm = w >> 1;
-    const uint32_t wread = (128 * wn + 8 * (col >> 2) + (col & 3)) * kBlock + ((grp ^ (col & 7)) << 4);   // (the key of that row: col & 7)
-    const uint32_t xread = (64 * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
-    int stage = 0;
     if (b0 >= total) return;
-    Place p = place(b0);
-    start(p);
-    fetch(0);
+    const int wn = w & 3, wm = w >> 2;
+    const uint32_t wread = (64 * wn + 8 * (col >> 2) + (col & 3)) * kBlock + ((grp ^ (col & 7)) << 4);   // (that row's key: col & 7)
+    const uint32_t xread = kTileBytes + (128 * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
+    const uint32_t sread = (128 * wm + col) * s_row;
+    int stage = 0;
+    Place here = place(b0), next = here;
+    start_w(here);
+    start_x(here);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fetch_w(0, i);
+    fetch_scales(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fetch_x(0, i);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fetch_w(1, i);
+    asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    int read_chunk = 1;
     for (int t = b0; t < total; t += G) {
-        const Place here = p;
-        const bool mine = here.r0 + 64 * wm < here.end && here.n0 + 128 * wn < a.N;
-        f32x4 acc[8][4];
+        const bool mine = here.r0 + 128 * wm < here.end && here.n0 + 64 * wn < a.N;
+        f32x4 acc[4][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int b = 0; b < kb; ++b) {
-            // this wavefront's part of the step has arrived and its reads of the step before are done; then everybody's
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            // This wavefront's part of the step has arrived (four loads, of weights for the next step, may be on their way; for a tile's
+            // first step that was waited for before the stores of the tile before) and its reads of the step before are done; then
+            // everybody's.
+            if (b == 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (b + 1 < kb) {
-                fetch(stage ^ 1);
-            } else if (t + G < total) {
-                p = place(t + G);
-                start(p);
-                fetch(stage ^ 1);
-            }
-            if (mine) {
-                const uint8_t *wt = lds + stage * kStageBytes, *xt = wt + kTileBytes;
-                const float *st = (const float *)(lds + kTileScales + stage * kStageScales);
-                float s[4];
+            if (b % kChunk == 0) read_chunk ^= 1;
+            const uint8_t *const st = lds + kTileScales + read_chunk * kChunkBytes + (b % kChunk) * s_block;
+            const uint8_t *const swt = lds + kTileScales + read_chunk * kChunkBytes + kChunk * kTile * 4 + (b % kChunk) * sw_block;
+            // (behind the last tile its own first steps are fetched once more and not read)
+            if (b + 1 == kb) start_x(next);
+            if (b + 1 == kb || (b + 1) % kChunk == 0) fetch_scales(b + 1 == kb ? 0 : b + 1);
+            if (b == 0 && t + G < total) next = place(t + G);
+            if (b + 2 == kb) start_w(next);
+            const uint8_t *const tile = lds + stage * kStageBytes;
+            // (fp32 results: the weights' wider operands in two passes, so that all stays in registers)
+            constexpr int P = OUT16 ? 1 : 2, I = 4 / P;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] = st[64 * wm + col + 16 * j] * st[kTile + wn];
-                // (fp32 results: the wider operands of two token groups at a time, so that all stays in registers)
-                constexpr int J = OUT16 ? 4 : 2;
+            for (int pass = 0; pass < P; ++pass) {
+                // The loads go out one at a time between the products: the loads of all wavefronts at once keep the address unit busy
+                // for a thousand cycles, in which a wavefront whose turn has not come issues nothing else.  The next step's rows first;
+                // then, when everybody has its weights (the products that read them are on their way), those of the step after next.
+                auto request = [&](int j) {
+                    if (pass == 0 && j < 4) fetch_x(stage ^ 1, j);
+                    if (pass == P - 1 && j >= 4) {
+                        if (j == 4) {
+                            __builtin_amdgcn_s_barrier();
+                            asm volatile("" ::: "memory");
+                        }
+                        fetch_w(stage, j - 4);
+                    }
+                };
+                if (!mine) {
 #pragma unroll
-                for (int j0 = 0; j0 < 4; j0 += J) {
-                    if (J < 4) {   // (read and convert again: nothing of the first pass is kept for the second)
-                        asm volatile("" ::: "memory");
+                    for (int j = 0; j < 8; ++j) request(j);
+                    continue;
+                }
+                u32x4 xraw[2], wraw[I][2];
+                auto read_x = [&](int j) {
+                    xraw[0] = *(const u32x4 *)(tile + xread + j * 16 * kBlock);
+                    xraw[1] = *(const u32x4 *)(tile + (xread ^ 64) + j * 16 * kBlock);
+                };
+                read_x(0);
+#pragma unroll
+                for (int i = 0; i < I; ++i) {
+                    const int at = ((pass * I + i) >> 1) * 32 + ((pass * I + i) & 1) * 4;
+                    wraw[i][0] = *(const u32x4 *)(tile + wread + at * kBlock);
+                    wraw[i][1] = *(const u32x4 *)(tile + (wread ^ 64) + at * kBlock);
+                }
+                auto scale = [&](int j) { return *(const float *)(st + sread + j * 16 * s_row); };
+                const float sw = *(const float *)(swt + (wn >> 1) * s_row);
+                Operand<!OUT16> wv[I];
+#pragma unroll
+                for (int i = 0; i < I; ++i) wv[i] = Operand<!OUT16>(wraw[i][0], wraw[i][1]);
+                // sixteen tokens' products while those before are scaled and added (in this order: left to itself the compiler puts
+                // every product's multiply-adds right behind it and waits)
+                f32x4 sum[2][I];
+                float s[2] = {scale(0) * sw, 0.f};
+#pragma unroll
+                for (int j = 0; j <= 8; ++j) {
+                    if (j < 8) request(j);
+                    const Operand<!OUT16> now(xraw[0], xraw[1]);
+                    float next_scale;
+                    if (j < 7) {
+                        read_x(j + 1);
+                        next_scale = scale(j + 1);
+                    }
+#pragma unroll
+                    for (int i = 0; i < I; ++i) {
+                        if (j < 8) sum[j & 1][i] = mfma128(wv[i], now);
+                        if (j > 0) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                acc[pass * I + i][j - 1][c] = __builtin_fmaf(sum[~j & 1][i][c], s[~j & 1], acc[pass * I + i][j - 1][c]);
+                        }
                         __builtin_amdgcn_sched_barrier(0);
                     }
-                    auto x = [&](int j) {
-                        const uint8_t *q = xt + (j0 + j) * 16 * kBlock;
-                        return Operand<!OUT16>(*(const u32x4 *)(q + xread), *(const u32x4 *)(q + (xread ^ 64)));
-                    };
-                    const Operand<!OUT16> xs[4] = {x(0), x(1), x(J == 4 ? 2 : 0), x(J == 4 ? 3 : 1)};
-                    auto y = [&](int i) {
-                        const uint8_t *q = wt + ((i >> 1) * 32 + (i & 1) * 4) * kBlock;
-                        return Operand<!OUT16>(*(const u32x4 *)(q + wread), *(const u32x4 *)(q + (wread ^ 64)));
-                    };
-                    // a weight operand's products while the ones before are scaled and added (in this order: left to itself the
-                    // compiler puts every product's multiply-adds right behind it and waits)
-                    f32x4 sum[2][J];
-                    Operand<!OUT16> ys = y(0);
-#pragma unroll
-                    for (int i = 0; i <= 8; ++i) {
-                        const Operand<!OUT16> now = ys;
-                        if (i < 7) ys = y(i + 1);
-#pragma unroll
-                        for (int j = 0; j < J; ++j) {
-                            if (i < 8) sum[i & 1][j] = mfma128(now, xs[j]);
-                            if (i > 0) {
-#pragma unroll
-                                for (int c = 0; c < 4; ++c)
-                                    acc[i - 1][j0 + j][c] = __builtin_fmaf(sum[~i & 1][j][c], s[j0 + j], acc[i - 1][j0 + j][c]);
-                            }
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
-                    }
+                    if (j < 7) s[~j & 1] = next_scale * sw;
                 }
             }
             stage ^= 1;
         }
+        asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = here.r0 + 64 * wm + 16 * j + col;
+        for (int j = 0; j < 8; ++j) {
+            const int r = here.r0 + 128 * wm + 16 * j + col;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int n = here.n0 + 128 * wn + 32 * i + 8 * grp;
+            for (int i = 0; i < 2; ++i) {
+                const int n = here.n0 + 64 * wn + 32 * i + 8 * grp;
                 if (r < here.end && n < a.N) {
                     const f32x4 u = acc[2 * i][j], v = acc[2 * i + 1][j];
                     if (OUT16) {
@@ -351,7 +410,9 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
                 }
             }
         }
+        here = next;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way to the LDS of a workgroup that has ended)
 }
 
 }  // namespace
@@ -366,8 +427,9 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
     if (!x || !x_scale || !w || !w_scale || !offsets || !out) return MOE_ERR_NULL;
     if (M < 1 || N < 1 || K < 1 || E < 1 || E > kMaxC || M > 1 << 30 || N > 1 << 24 || K > 1 << 20) return MOE_ERR_SHAPE;
     if (N % 8 || K % kBlock || !aligned16(x) || !aligned16(w) || !aligned16(out)) return MOE_ERR_ALIGN;
-    MatmulArgs a = {(const uint8_t *)x, (const uint8_t *)w, x_scale, w_scale, offsets, out, M, N, K, E};
-    if (M / E >= 64) {
+    MatmulArgs a = {(const uint8_t *)x, (const uint8_t *)w, x_scale, w_scale, offsets, out, M, N, K, E,
+                    K / kBlock % 4 == 0 && aligned16(x_scale) && aligned16(w_scale)};
+    if (M / E >= 64 && K > kBlock) {
         hipError_t err;
         const int cus = device_cus(&err);
         if (err != hipSuccess) return launch_failed(err);
