@@ -169,6 +169,33 @@ def test_product_long_sums_many_experts_many_rows(counts, N, K, dtype):
     _check(*_operands(counts, N, K, 11), dtype)
 
 
+# many rows to an expert and enough of them to fill the device: rows that end anywhere in a tile of 256, widths that end inside one,
+# two blocks of columns and more, scales that are whole 16-byte words and not
+MANY = [([7 * i * i % 83 for i in range(40)], 1000, 1000), ([7 * i * i % 83 for i in range(40)], 1040, 1408), ([700, 0, 1300], 4104, 640),
+        ([5000], 2056, 256), ([0, 3000, 1, 2049], 2312, 384), ([16, 17, 0, 15, 1, 255, 256, 257] * 4, 1032, 512), ([9] * 300, 264, 2176)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("counts,N,K", MANY, ids=[f"{sum(c)}in{len(c)}x{n}x{k}" for c, n, k in MANY])
+def test_product_many_rows(counts, N, K, dtype):
+    _check(*_operands(counts, N, K, 12), dtype)
+
+
+def test_many_rows_rows_of_no_expert_and_nan():
+    a, sa, w, sw, offsets = _operands([300, 0, 700], 4104, 512, 13, lead=5, tail=30)
+    _check(a, sa, w, sw, offsets, torch.bfloat16)
+    clean = _run(a, sa, w, sw, offsets, torch.bfloat16)
+    assert torch.equal(clean, _run(a, sa, w, sw, offsets, torch.bfloat16))
+    a.view(torch.uint8)[4, 300] = 0x7f        # of no expert
+    a.view(torch.uint8)[304, 300] = 0x7f      # the last row of the first
+    sa[700, 1] = float("nan")
+    w.view(torch.uint8)[2, 4103, 0] = 0xff
+    got = _run(a, sa, w, sw, offsets, torch.bfloat16)
+    bad = torch.zeros(got.shape, dtype=torch.bool)
+    bad[304], bad[700], bad[305:1005, 4103] = True, True, True
+    assert bool(torch.isnan(got[bad]).all()) and torch.equal(got[~bad], clean[~bad])
+
+
 @pytest.mark.parametrize("lead,tail", [(0, 9), (5, 0), (3, 40)])
 def test_rows_of_no_expert_are_left(lead, tail):
     for counts in ([4, 0, 19], [0, 0, 0], [90, 200]):
