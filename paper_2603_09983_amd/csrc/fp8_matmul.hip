@@ -207,9 +207,9 @@ __global__ __launch_bounds__((kMostWaves<OUT16, T>)*kWave) void stream_matmul_ke
     }
 }
 
-// ---- many rows to an expert: tiles of 256 weight rows x 256 tokens through LDS ----
+// ---- many rows to an expert: tiles of 256 weight rows x 256 tokens (or 128) through LDS ----
 // Bound by the matrix cores.  One workgroup of eight wavefronts per CU walks the tiles; a step is one block of 128 columns, 32 KB of
-// weights and 32 KB of rows.  A wavefront has 64 weight rows x 128 tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core)
+// weights and 32 (16) KB of rows.  A wavefront has 64 weight rows x 128 (64) tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core)
 // four multiply-adds (16 cycles of the vector ALU) bring the block's sum, times its scales, into the tile's.
 //
 // LDS holds two steps.  A wavefront reads its weights of a step at its beginning and keeps them; once all have (a second barrier), the
@@ -219,13 +219,16 @@ __global__ __launch_bounds__((kMostWaves<OUT16, T>)*kWave) void stream_matmul_ke
 //
 // A row's eight 16-byte words are permuted by a key of the row, so that the eight lanes that a read serves at a time find eight
 // different words.  Weight rows go to the matrix rows so that a lane's results of two products are eight consecutive columns of `out`.
-constexpr int kTile = 256, kTileThreads = 512;
-constexpr int kTileBytes = kTile * kBlock, kStageBytes = 2 * kTileBytes;
+constexpr int kTile = 256, kTileThreads = 512;             // weight rows of a tile
+constexpr int kTileBytes = kTile * kBlock;
 constexpr int kChunk = 4;                                  // blocks whose scales are fetched together
-constexpr int kChunkBytes = kChunk * (kTile + kWave) * 4;  // of 256 tokens, then of the two blocks of weight rows (and padding)
-constexpr int kTileScales = 2 * kStageBytes, kTileTable = kTileScales + 2 * kChunkBytes;
-constexpr int kTileLds = kTileTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
-static_assert(kTileLds <= kLdsBytes, "two stages, their scales, the experts' first tiles");
+constexpr int kChunkBytes = kChunk * (kTile + kWave) * 4;  // of the tokens, then of the two blocks of weight rows (and padding)
+template <int J>   // tokens of a tile: 32 J
+struct TileSize {
+    static constexpr int kTokens = 32 * J, kStage = kTileBytes + kTokens * kBlock;
+    static constexpr int kScales = 2 * kStage, kTable = kScales + 2 * kChunkBytes, kLds = kTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
+    static_assert(kLds <= kLdsBytes, "two stages, their scales, the experts' first tiles");
+};
 
 // 16 (or 4) bytes a lane from base + at to LDS, lane after lane from `to` on.  Not waited for by the compiler: the loop counts.
 __device__ __forceinline__ void fetch16(uint32_t to, uint32_t at, const void *base)
@@ -237,11 +240,11 @@ __device__ __forceinline__ void fetch4(uint32_t to, uint32_t at, const void *bas
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
 }
 
-// first[e] = tiles of 256 rows of the experts before e, e = 0..E (all threads of a workgroup; E <= 2 * threads).  No more than there
-// can be where no expert's rows are another's too.
-__device__ __forceinline__ void count_tiles(const int32_t *offsets, int M, int E, int32_t *first, int32_t *wave_sum)
+// first[e] = tiles of `tokens` rows of the experts before e, e = 0..E (all threads of a workgroup; E <= 2 * threads).  No more than
+// there can be where no expert's rows are another's too.
+__device__ __forceinline__ void count_tiles(int tokens, const int32_t *offsets, int M, int E, int32_t *first, int32_t *wave_sum)
 {
-    const int most = (M + kTile - 1) / kTile + (E < M ? E : M);
+    const int most = (M + tokens - 1) / tokens + (E < M ? E : M);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
     int n[2];
 #pragma unroll
@@ -250,7 +253,7 @@ __device__ __forceinline__ void count_tiles(const int32_t *offsets, int M, int E
         n[i] = 0;
         if (e < E) {
             const int rows = clamped(offsets[e + 1], M) - clamped(offsets[e], M);
-            n[i] = rows > 0 ? (rows + kTile - 1) / kTile : 0;
+            n[i] = rows > 0 ? (rows + tokens - 1) / tokens : 0;
         }
     }
     int up = n[0] + n[1];
@@ -271,14 +274,15 @@ __device__ __forceinline__ void count_tiles(const int32_t *offsets, int M, int E
     __syncthreads();
 }
 
-template <bool OUT16>
+template <bool OUT16, int J>
 __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
 {
+    constexpr int kTokens = TileSize<J>::kTokens, kStageBytes = TileSize<J>::kStage, kTileScales = TileSize<J>::kScales;
     extern __shared__ __align__(16) uint8_t lds[];
-    int32_t *first = (int32_t *)(lds + kTileTable);
+    int32_t *first = (int32_t *)(lds + TileSize<J>::kTable);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock, tiles_n = (a.N + kTile - 1) / kTile, nb = (a.N + kBlock - 1) / kBlock;
-    count_tiles(a.offsets, a.M, a.E, first, first + kMaxC + 1);
+    count_tiles(kTokens, a.offsets, a.M, a.E, first, first + kMaxC + 1);
     const int total = __builtin_amdgcn_readfirstlane(first[a.E]) * tiles_n;
 
     // Where a tile lies.  An expert's tiles: its row tiles first, then the next 256 weight rows.
@@ -292,14 +296,14 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
         const int f = __builtin_amdgcn_readfirstlane(first[e]), m = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
         const int local = t - f * tiles_n, n = local / m;
         const int lo = clamped(a.offsets[e], a.M), hi = clamped(a.offsets[e + 1], a.M);
-        return Place{e, n * kTile, lo + (local - n * m) * kTile, hi};
+        return Place{e, n * kTile, lo + (local - n * m) * kTokens, hi};
     };
 
     // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word each.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
     const int frow = tid / 8, wkey = (frow & 3) | ((frow >> 1) & 4), xkey = frow & 7;
     const uint8_t *wbase, *xbase;
-    uint32_t wat[4], xat[4];
+    uint32_t wat[4], xat[J / 2];
     auto start_w = [&](const Place &p) {
         wbase = a.w + ((size_t)p.e * a.N + p.n0) * a.K;
 #pragma unroll
@@ -320,7 +324,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     auto start_x = [&](const Place &p) {
         xbase = a.a + (size_t)p.r0 * a.K;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < J / 2; ++i) {
             const int r = frow + 64 * i < p.end - p.r0 ? frow + 64 * i : p.end - p.r0 - 1;
             xat[i] = (uint32_t)r * a.K + ((tid & 7) ^ xkey) * 16;
         }
@@ -335,7 +339,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     };
     auto fetch_x = [&](int stage, int i) {
         fetch16(lds0 + stage * kStageBytes + kTileBytes + w * 1024 + i * 8192, xat[i], xbase);
-        if (i == 3) xbase += kBlock;
+        if (i == J / 2 - 1) xbase += kBlock;
     };
     int chunk = 1;   // which half of the scales' place holds the chunk fetched last
     auto fetch_scales = [&](int b) {   // of blocks b .. b + 3
@@ -354,8 +358,8 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     if (b0 >= total) return;
     const int wn = w & 3, wm = w >> 2;
     const uint32_t wread = (64 * wn + 8 * (col >> 2) + (col & 3)) * kBlock + ((grp ^ (col & 7)) << 4);   // (that row's key: col & 7)
-    const uint32_t xread = kTileBytes + (128 * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
-    const uint32_t sread = (128 * wm + col) * s_row;
+    const uint32_t xread = kTileBytes + (16 * J * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
+    const uint32_t sread = (16 * J * wm + col) * s_row;
     int stage = 0;
     Place here = place(b0), next = here;
     start_w(here);
@@ -364,18 +368,18 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     for (int i = 0; i < 4; ++i) fetch_w(0, i);
     fetch_scales(0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) fetch_x(0, i);
+    for (int i = 0; i < J / 2; ++i) fetch_x(0, i);
 #pragma unroll
     for (int i = 0; i < 4; ++i) fetch_w(1, i);
     asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
     int read_chunk = 1;
     for (int t = b0; t < total; t += G) {
-        const bool mine = here.r0 + 128 * wm < here.end && here.n0 + 64 * wn < a.N;
-        f32x4 acc[4][8];
+        const bool mine = here.r0 + 16 * J * wm < here.end && here.n0 + 64 * wn < a.N;
+        f32x4 acc[4][J];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < J; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         for (int b = 0; b < kb; ++b) {
             // This wavefront's part of the step has arrived (four loads, of weights for the next step, may be on their way; for a tile's
             // first step that was waited for before the stores of the tile before) and its reads of the step before are done; then
@@ -401,18 +405,19 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
                 // for a thousand cycles, in which a wavefront whose turn has not come issues nothing else.  The next step's rows first;
                 // then, when everybody has its weights (the products that read them are on their way), those of the step after next.
                 auto request = [&](int j) {
-                    if (pass == 0 && j < 4) fetch_x(stage ^ 1, j);
-                    if (pass == P - 1 && j >= 4) {
-                        if (j == 4) {
+                    if (pass == 0 && j < J / 2) fetch_x(stage ^ 1, j);
+                    if (pass == P - 1 && j >= J / 2) {
+                        if (j == J / 2) {
                             __builtin_amdgcn_s_barrier();
                             asm volatile("" ::: "memory");
                         }
-                        fetch_w(stage, j - 4);
+#pragma unroll
+                        for (int i = 0; i < 8 / J; ++i) fetch_w(stage, (j - J / 2) * (8 / J) + i);
                     }
                 };
                 if (!mine) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) request(j);
+                    for (int j = 0; j < J; ++j) request(j);
                     continue;
                 }
                 u32x4 xraw[2], wraw[I][2];
@@ -437,17 +442,17 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
                 f32x4 sum[2][I];
                 float s[2] = {scale(0) * sw, 0.f};
 #pragma unroll
-                for (int j = 0; j <= 8; ++j) {
-                    if (j < 8) request(j);
+                for (int j = 0; j <= J; ++j) {
+                    if (j < J) request(j);
                     const Operand<!OUT16> now(xraw[0], xraw[1]);
                     float next_scale;
-                    if (j < 7) {
+                    if (j < J - 1) {
                         read_x(j + 1);
                         next_scale = scale(j + 1);
                     }
 #pragma unroll
                     for (int i = 0; i < I; ++i) {
-                        if (j < 8) sum[j & 1][i] = mfma128(wv[i], now);
+                        if (j < J) sum[j & 1][i] = mfma128(wv[i], now);
                         if (j > 0) {
 #pragma unroll
                             for (int c = 0; c < 4; ++c)
@@ -455,15 +460,15 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
-                    if (j < 7) s[~j & 1] = next_scale * sw;
+                    if (j < J - 1) s[~j & 1] = next_scale * sw;
                 }
             }
             stage ^= 1;
         }
         asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = here.r0 + 128 * wm + 16 * j + col;
+        for (int j = 0; j < J; ++j) {
+            const int r = here.r0 + 16 * J * wm + 16 * j + col;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int n = here.n0 + 64 * wn + 32 * i + 8 * grp;
@@ -503,12 +508,22 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
     const int cus = device_cus(&err);
     if (err != hipSuccess) return launch_failed(err);
     const size_t experts = E < M ? E : M;
-    const size_t tiles = ((size_t)(M + kTile - 1) / kTile + experts) * ((N + kTile - 1) / kTile);   // (at most)
-    if (tiles >= (size_t)1 << 30) return MOE_ERR_SHAPE;
+    // Which kernel, by the mean number of rows an expert has (64 experts of 2816 x 2048, us; 40 of 2040 x 1000 in brackets):
+    //   rows          6     12    24 (25)    47     94    187    281    768
+    //   streaming    60     80   135 (42)   234      -      -      -      -
+    //   128 tokens   70     70    73 (16)    78     89    134    169    363
+    //   256 tokens   74     75    78 (20)    83     91    119    182    334
+    // Tiles that would leave half of the device idle are left to the streaming kernel, which cuts the work finer.
     const bool few = M / E < 8;
-    if (!few && K > kBlock && tiles >= (size_t)cus / 2)
-        return launch_rows(out_bf16 ? (const void *)tile_matmul_kernel<true> : (const void *)tile_matmul_kernel<false>,
-                           dim3(tiles < (size_t)cus ? (unsigned)tiles : cus), kTileThreads, &a, kTileLds, stream, MOE_KERNEL_MATMUL);
+    const int tokens = M / E <= 128 ? 128 : 256;
+    const size_t tiles = ((size_t)(M + tokens - 1) / tokens + experts) * ((N + kTile - 1) / kTile);   // (at most)
+    if (tiles >= (size_t)1 << 30) return MOE_ERR_SHAPE;
+    if (!few && K > kBlock && tiles >= (size_t)cus / 2) {
+        const void *fn = tokens == 128 ? (out_bf16 ? (const void *)tile_matmul_kernel<true, 4> : (const void *)tile_matmul_kernel<false, 4>)
+                                       : (out_bf16 ? (const void *)tile_matmul_kernel<true, 8> : (const void *)tile_matmul_kernel<false, 8>);
+        return launch_rows(fn, dim3(tiles < (size_t)cus ? (unsigned)tiles : cus), kTileThreads, &a,
+                           tokens == 128 ? TileSize<4>::kLds : TileSize<8>::kLds, stream, MOE_KERNEL_MATMUL);
+    }
     // sixteen wavefronts to a CU, as far as the columns go round
     const size_t groups = experts * ((N + 31) / 32);
     const int most = few && out_bf16 ? kMostWaves<true, 1> : kMostWaves<false, 1>;
