@@ -18,7 +18,7 @@ struct QuantArgs {
     const int32_t *n_rows;      // [1] or null: rows from *n_rows on are left as they are
     u32x4 *q;                   // [M,Kp]
     float *scale;               // [M,Kb]
-    int M, K;
+    int M, K, stream;
     unsigned blocks, rcp_blocks, items;
 };
 
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(QuantArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) m = larger(m, magnitude(f[i]));
         const float top = __uint_as_float(largest_of_8(m));
-        a.q[(size_t)g * 8 + sub] = sixteen_fp8(f, kTop / top);
+        put(a.q + (size_t)g * 8 + sub, sixteen_fp8(f, kTop / top), a.stream);
         if (sub == 0) a.scale[g] = top / kTop;
     }
 }
@@ -74,7 +74,7 @@ struct QuantWeightArgs {
     const void *w;              // [E,N,K]
     u32x4 *q;                   // [E,N,Kp]
     float *scale;               // [E,Nb,Kb]
-    int N, K;
+    int N, K, stream;
     unsigned nb, kb, rcp_nb, rcp_kb, items;
 };
 
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_weights_kernel(QuantWe
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int n = (int)nb * kBlock + i * 32 + tid / 8;
-            if (n < a.N) a.q[(((size_t)e * a.N + n) * a.kb + b) * 8 + sub] = sixteen_fp8(f[i], by);
+            if (n < a.N) put(a.q + (((size_t)e * a.N + n) * a.kb + b) * 8 + sub, sixteen_fp8(f[i], by), a.stream);
         }
         if (tid == 0) a.scale[item] = top / kTop;
     }
@@ -122,7 +122,8 @@ int quantize_rows(const void *x, int x_bf16, const int32_t *n_rows, int M, int K
     if (!x || !q || !scale) return MOE_ERR_NULL;
     if (M < 1 || K < 1 || M > 1 << 30 || K > 1 << 24) return MOE_ERR_SHAPE;
     if (K % 8 || !aligned16(x) || !aligned16(q)) return MOE_ERR_ALIGN;
-    QuantArgs a = {x, n_rows, (u32x4 *)q, scale, M, K, (unsigned)((K + kBlock - 1) / kBlock), 0, 0};
+    QuantArgs a = {x, n_rows, (u32x4 *)q, scale, M, K, 0, (unsigned)((K + kBlock - 1) / kBlock), 0, 0};
+    a.stream = (size_t)M * a.blocks * kBlock > kStreamBytes;
     const size_t items = (size_t)M * a.blocks;
     if (items >= (size_t)1 << 31) return MOE_ERR_SHAPE;
     a.rcp_blocks = rcp32(a.blocks);
@@ -154,7 +155,8 @@ extern "C" int moe_quantize_weights_fp8(const void *w, int w_bf16, int E, int N,
     if (!w || !q || !scale) return MOE_ERR_NULL;
     if (E < 1 || N < 1 || K < 1 || E > kMaxC || N > 1 << 24 || K > 1 << 24) return MOE_ERR_SHAPE;
     if (K % 8 || !aligned16(w) || !aligned16(q)) return MOE_ERR_ALIGN;
-    QuantWeightArgs a = {w, (u32x4 *)q, scale, N, K, (unsigned)((N + kBlock - 1) / kBlock), (unsigned)((K + kBlock - 1) / kBlock), 0, 0, 0};
+    QuantWeightArgs a = {w, (u32x4 *)q, scale, N, K, 0, (unsigned)((N + kBlock - 1) / kBlock), (unsigned)((K + kBlock - 1) / kBlock), 0, 0, 0};
+    a.stream = (size_t)E * N * a.kb * kBlock > kStreamBytes;
     const size_t items = (size_t)E * a.nb * a.kb;
     if (items >= (size_t)1 << 31) return MOE_ERR_SHAPE;
     a.rcp_nb = rcp32(a.nb);

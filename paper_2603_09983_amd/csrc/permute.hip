@@ -16,7 +16,8 @@ using namespace rows;
 // ---- sort ----
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortBlocks = 128;      // most workgroups of the two-launch form
-constexpr int kSortChunk = 2048;      // least assignments of one of its workgroups
+constexpr int kSortChunk = 1024;      // least assignments of one of its workgroups (98304 on 64 experts: 8.2 us; 2048 8.4, 4096 8.9)
+constexpr int kAhead = 4;             // loads in flight
 constexpr int kSortOne = 4096;        // up to so many assignments: one workgroup, one launch
 
 struct SortArgs {
@@ -65,20 +66,32 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
     const int begin = blockIdx.x * a.chunk, end = begin + a.chunk < a.A ? begin + a.chunk : a.A;
     const int per_wave = a.chunk / kSortWaves;      // (a multiple of 64)
     const int first = begin + w * per_wave, last = first + per_wave < end ? first + per_wave : end;
-    for (int i = first; i < last; i += kWave) {
-        const int e = expert_of(a, i + lane, last);
-        if (e >= 0) atomicAdd(&part[w * a.E + e], 1);
+    for (int i = first; i < last; i += kAhead * kWave) {
+        int e[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) e[u] = expert_of(a, i + u * kWave + lane, last);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (e[u] >= 0) atomicAdd(&part[w * a.E + e[u]], 1);
     }
     if (!ONE) {
-        // the counts of all chunks: sixteen rows of the table at a time, a wavefront a row
-        for (int b = w; b < a.blocks; b += kSortWaves)
-            for (int e = lane; e < a.E; e += kWave) {
-                const int n = a.counts[(size_t)b * a.E + e];
-                if (n) {
-                    atomicAdd(&all[e], n);
-                    if (b < (int)blockIdx.x) atomicAdd(&before[e], n);
+        // the counts of all chunks: a wavefront has every sixteenth row of the table
+        for (int e0 = lane; e0 < a.E; e0 += kAhead * kWave) {
+            int n[kAhead] = {}, m[kAhead] = {};
+#pragma unroll 4
+            for (int b = w; b < a.blocks; b += kSortWaves)
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    const int e = e0 + u * kWave, c = e < a.E ? a.counts[(size_t)b * a.E + e] : 0;
+                    n[u] += c;
+                    m[u] += b < (int)blockIdx.x ? c : 0;
                 }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (n[u]) atomicAdd(&all[e0 + u * kWave], n[u]);
+                if (m[u]) atomicAdd(&before[e0 + u * kWave], m[u]);
             }
+        }
     }
     __syncthreads();
     // E <= 1024 = threads: thread e has expert e
@@ -112,25 +125,32 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
     if (blockIdx.x == 0 && tid == 0) a.offsets[a.E] = valid;
     for (int r = valid + blockIdx.x * kSortThreads + tid; r < a.A; r += gridDim.x * kSortThreads) a.order[r] = -1;
     __syncthreads();
-    for (int i = first; i < last; i += kWave) {
-        const int e = expert_of(a, i + lane, last);
-        unsigned long long same = __ballot(e >= 0);
-        for (int b = 0; b < a.bits; ++b) {
-            const unsigned long long set = __ballot((e >> b) & 1);
-            same &= (e >> b) & 1 ? set : ~set;
+    for (int i = first; i < last; i += kAhead * kWave) {
+        int e[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) e[u] = expert_of(a, i + u * kWave + lane, last);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int at = i + u * kWave;
+            if (at >= last) break;
+            unsigned long long same = __ballot(e[u] >= 0);
+            for (int b = 0; b < a.bits; ++b) {
+                const unsigned long long set = __ballot((e[u] >> b) & 1);
+                same &= (e[u] >> b) & 1 ? set : ~set;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1ull));
+            int place = -1;
+            if (e[u] >= 0) {
+                place = part[w * a.E + e[u]] + rank;
+                a.order[place] = at + lane;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (every lane has read its place before the first of them moves on)
+            __builtin_amdgcn_wave_barrier();
+            if (e[u] >= 0 && rank == 0) part[w * a.E + e[u]] += __popcll(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (at + lane < last) a.pos[at + lane] = place;
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1ull));
-        int place = -1;
-        if (e >= 0) {
-            place = part[w * a.E + e] + rank;
-            a.order[place] = i + lane;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (every lane has read its place before the first of them moves on)
-        __builtin_amdgcn_wave_barrier();
-        if (e >= 0 && rank == 0) part[w * a.E + e] += __popcll(same);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (i + lane < last) a.pos[i + lane] = place;
     }
 }
 
@@ -149,7 +169,7 @@ struct MoveArgs {
     const u32x4 *x;          // [T] rows of `words` words
     const int32_t *pos;      // [T,k]
     u32x4 *out;              // [R]
-    int k, R, words;
+    int k, R, words, stream;
     unsigned parts, rcp_parts, items;
 };
 
@@ -172,7 +192,7 @@ __global__ __launch_bounds__(kRowThreads) void permute_kernel(MoveArgs a)
             u32x4 *dst = a.out + (size_t)r * a.words;
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (c0 + u * kWave < a.words) dst[c0 + u * kWave] = v[u];
+                if (c0 + u * kWave < a.words) put(dst + c0 + u * kWave, v[u], a.stream);
         }
     }
 }
@@ -182,7 +202,7 @@ struct MoveFp8Args {
     const int32_t *pos;
     u32x4 *q;                // [R,Hp]
     float *scale;            // [R,Hb]
-    int T, k, R, H;
+    int k, R, H, stream;
     unsigned blocks, rcp_blocks, items;   // blocks of a row; T * blocks
 };
 
@@ -212,7 +232,7 @@ __global__ __launch_bounds__(kRowThreads) void permute_fp8_kernel(MoveFp8Args a)
         for (int j = 0; j < a.k; ++j) {
             const int r = a.pos[(size_t)t * a.k + j];
             if ((unsigned)r >= (unsigned)a.R) continue;
-            a.q[((size_t)r * a.blocks + b) * 8 + sub] = q;
+            put(a.q + ((size_t)r * a.blocks + b) * 8 + sub, q, a.stream);
             if (sub == 0) a.scale[(size_t)r * a.blocks + b] = scale;
         }
     }
@@ -223,7 +243,7 @@ struct SumArgs {
     const int32_t *pos;      // [T,k]
     const float *w;          // [T,k] or null (ones)
     u32x4 *out;              // [T,H]
-    int k, R, H, accumulate;
+    int k, R, H, accumulate, stream;
     unsigned parts, rcp_parts, items;
 };
 
@@ -239,13 +259,13 @@ __device__ __forceinline__ void load8(const u32x4 *row, int unit, float *f)
     }
 }
 template <bool BF16>
-__device__ __forceinline__ void store8(u32x4 *row, int unit, const float *f)
+__device__ __forceinline__ void store8(u32x4 *row, int unit, const float *f, int stream)
 {
     if (BF16) {
-        row[unit] = to_word<true>(f);
+        put(row + unit, to_word<true>(f), stream);
     } else {
-        row[2 * unit] = to_word<false>(f);
-        row[2 * unit + 1] = to_word<false>(f + 4);
+        put(row + 2 * unit, to_word<false>(f), stream);
+        put(row + 2 * unit + 1, to_word<false>(f + 4), stream);
     }
 }
 
@@ -274,7 +294,7 @@ __global__ __launch_bounds__(kRowThreads) void unpermute_kernel(SumArgs a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(by, f[i], sum[i]);
         }
-        store8<OUT16>(out, unit, sum);
+        store8<OUT16>(out, unit, sum, a.stream);
     }
 }
 
@@ -285,7 +305,7 @@ struct BackArgs {
     const float *w;          // [T,k] or null
     u32x4 *drows;            // [R,H] or null
     float *dw;               // [T,k] or null
-    int k, R, H;
+    int k, R, H, stream;
     unsigned A, rcp_k;
 };
 
@@ -318,7 +338,7 @@ __global__ __launch_bounds__(kRowThreads) void unpermute_backward_kernel(BackArg
             if (a.drows) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) g[c] *= by;
-                store8<IN16>(a.drows + (size_t)r * (a.H / nin), unit, g);
+                store8<IN16>(a.drows + (size_t)r * (a.H / nin), unit, g, a.stream);
             }
         }
         if (a.dw) {
@@ -385,7 +405,8 @@ extern "C" int moe_permute(const void *x, int x_bf16, const int32_t *pos, int T,
     int rc = check_rows(T, k, H, R);
     if (rc) return rc;
     if (!aligned16(x) || !aligned16(out)) return MOE_ERR_ALIGN;
-    MoveArgs a = {(const u32x4 *)x, pos, (u32x4 *)out, k, R, x_bf16 ? H / 8 : H / 4, 0, 0, 0};
+    MoveArgs a = {(const u32x4 *)x, pos, (u32x4 *)out, k, R, x_bf16 ? H / 8 : H / 4, 0, 0, 0, 0};
+    a.stream = (size_t)T * k * a.words * 16 > kStreamBytes;
     auto parts = [&](int U) { return (unsigned)((a.words + U * kWave - 1) / (U * kWave)); };
     const int U = (size_t)T * parts(4) >= 1024 ? 4 : 1;
     a.parts = parts(U);
@@ -404,7 +425,8 @@ extern "C" int moe_permute_fp8(const void *x, int x_bf16, const int32_t *pos, in
     int rc = check_rows(T, k, H, R);
     if (rc) return rc;
     if (!aligned16(x) || !aligned16(q)) return MOE_ERR_ALIGN;
-    MoveFp8Args a = {x, pos, (u32x4 *)q, scale, T, k, R, H, (unsigned)((H + kBlock - 1) / kBlock), 0, 0};
+    MoveFp8Args a = {x, pos, (u32x4 *)q, scale, k, R, H, 0, (unsigned)((H + kBlock - 1) / kBlock), 0, 0};
+    a.stream = (size_t)T * k * a.blocks * kBlock > kStreamBytes;
     const size_t items = (size_t)T * a.blocks;
     if (items >= (size_t)1 << 31) return MOE_ERR_SHAPE;
     a.rcp_blocks = rcp32(a.blocks);
@@ -420,7 +442,8 @@ extern "C" int moe_unpermute(const void *rows, int rows_bf16, const int32_t *pos
     int rc = check_rows(T, k, H, R);
     if (rc) return rc;
     if (!aligned16(rows) || !aligned16(out)) return MOE_ERR_ALIGN;
-    SumArgs a = {(const u32x4 *)rows, pos, topk_w, (u32x4 *)out, k, R, H, accumulate, (unsigned)((H / 8 + kWave - 1) / kWave), 0, 0};
+    SumArgs a = {(const u32x4 *)rows, pos, topk_w, (u32x4 *)out, k, R, H, accumulate,
+                 (size_t)T * H * (out_bf16 ? 2 : 4) > kStreamBytes, (unsigned)((H / 8 + kWave - 1) / kWave), 0, 0};
     const size_t items = (size_t)T * a.parts;
     if (items >= (size_t)1 << 31) return MOE_ERR_SHAPE;
     a.rcp_parts = rcp32(a.parts);
@@ -437,7 +460,8 @@ extern "C" int moe_unpermute_backward(const void *dout, int dout_bf16, const voi
     int rc = check_rows(T, k, H, R);
     if (rc) return rc;
     if (!aligned16(dout) || !aligned16(rows) || !aligned16(drows)) return MOE_ERR_ALIGN;
-    BackArgs a = {(const u32x4 *)dout, (const u32x4 *)rows, pos, topk_w, (u32x4 *)drows, dtopk_w, k, R, H, (unsigned)T * (unsigned)k,
+    BackArgs a = {(const u32x4 *)dout, (const u32x4 *)rows, pos, topk_w, (u32x4 *)drows, dtopk_w, k, R, H,
+                  (size_t)T * k * H * (rows_bf16 ? 2 : 4) > kStreamBytes, (unsigned)T * (unsigned)k,
                   rcp32((unsigned)k)};
     const void *fn = dout_bf16 ? (rows_bf16 ? (const void *)unpermute_backward_kernel<true, true> : (const void *)unpermute_backward_kernel<true, false>)
                                : (rows_bf16 ? (const void *)unpermute_backward_kernel<false, true> : (const void *)unpermute_backward_kernel<false, false>);
