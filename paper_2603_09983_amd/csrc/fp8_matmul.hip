@@ -397,8 +397,8 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
             if (b == 0 && t + G < total) next = place(t + G);
             if (b + 2 == kb) start_w(next);
             const uint8_t *const tile = lds + stage * kStageBytes;
-            // (fp32 results: the weights' wider operands in two passes, so that all stays in registers)
-            constexpr int P = OUT16 ? 1 : 2, I = 4 / P;
+            // (fp32 results of 256 tokens: the weights' wider operands in two passes, so that all stays in registers)
+            constexpr int P = OUT16 || J == 4 ? 1 : 2, I = 4 / P;
 #pragma unroll
             for (int pass = 0; pass < P; ++pass) {
                 // The loads go out one at a time between the products: the loads of all wavefronts at once keep the address unit busy
