@@ -81,7 +81,8 @@ __device__ __forceinline__ f32x4 mfma128(const Operand<true> &a, const Operand<t
 // ---- few rows to an expert: its weights streamed past them ----
 // Bound by the weights' bytes.  A workgroup has 32 weight rows of one expert against its tokens, 16 T at a time; its wavefronts share
 // the columns, block by block (neighbouring wavefronts have neighbouring blocks: together they read consecutive columns), and their
-// sums meet in LDS in a fixed order.  Each has U blocks in flight: 32 rows x 128 columns of weights, 16 T x 128 of rows (which all
+// sums meet in LDS in a fixed order.  gridDim.z workgroups take an expert's tokens in turn, so that an expert that has many (routing is
+// uneven, and the host does not know how) does not keep everybody waiting.  A wavefront has U blocks in flight: 32 rows x 128 columns of weights, 16 T x 128 of rows (which all
 // workgroups of the expert read: from L2).
 template <bool OUT16, int T>
 constexpr int kMostWaves = OUT16 && T == 1 ? 16 : 8;   // (so that what is in flight has the registers)
@@ -119,7 +120,7 @@ __global__ __launch_bounds__((kMostWaves<OUT16, T>)*kWave) void stream_matmul_ke
         if (e < 0) return;
     }
     const int lo = clamped(a.offsets[e], a.M), hi = clamped(a.offsets[e + 1], a.M);
-    if (lo >= hi) return;
+    if (lo + (int)blockIdx.z * 16 * T >= hi) return;
     const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock;
     const uint8_t *wrow[4];
@@ -130,7 +131,7 @@ __global__ __launch_bounds__((kMostWaves<OUT16, T>)*kWave) void stream_matmul_ke
     }
     const bool upper = col >= 8;
     const float *const sw = a.w_scale + ((size_t)e * ((a.N + kBlock - 1) / kBlock) + n0 / kBlock) * kb;
-    for (int r0 = lo; r0 < hi; r0 += 16 * T) {
+    for (int r0 = lo + (int)blockIdx.z * 16 * T; r0 < hi; r0 += (int)gridDim.z * 16 * T) {
         const uint8_t *xrow[T];
         const float *sx[T];
 #pragma unroll
@@ -490,6 +491,57 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way to the LDS of a workgroup that has ended)
 }
 
+// Which kernel takes a call: the one that should be the fastest by what they measured, from the sizes alone (the mean number of rows an
+// expert has, r).  us; 64 experts of 2816 x 2048 where nothing else is said, bf16 results:
+//      r                  6     12     24     47     94    187    281    768     64 (one expert)  12 (8 of 448 x 5664)  364 (8 of 328 x 5176)
+//      streaming, 16     60     82    148    262      -      -      -      -     20                12                     -
+//      streaming, 64     86     92    108    142      -      -      -      -     11                14                     111
+//      tiles of 128      69     70     73     78     89    134    169    363     16                35                     47
+//      tiles of 256      73     75     78     82     91    119    182    334     20                47                     65
+// The streaming kernels: so many passes over an expert's rows, each bound by the weights' bytes (6 TB/s) or by the blocks that a wavefront
+// loads one after the other (1.6 us; as much again for 64 rows that differ, up to seven wavefronts a CU).
+// The tiles: rounds of them over the CUs, each as many steps as there are blocks, a step's time by how many of its rows there are; or
+// the weights' bytes again (5.3 TB/s).
+struct Choice {
+    int tokens;          // 16, 64: the streaming kernel; 128, 256: tiles
+    int waves, depth;    // the streaming kernel's wavefronts, and workgroups to an expert's rows
+};
+
+Choice choose(int M, int N, int K, int E, bool out16, int cus)
+{
+    const double kb = K / kBlock, experts = E < M ? E : M, r = M / experts, groups = experts * ((N + 31) / 32);
+    const double megabytes = experts * N * K * 1e-6;
+    auto waves = [&](int most) {   // sixteen to a CU, as far as the columns go round
+        int w = 4;
+        while (w < most && groups * w < cus * 16.0 && kb >= 2 * w) w *= 2;
+        return w;
+    };
+    auto up = [](double x) { return (double)(long long)(x + 0.999999); };
+    auto least = [](double a, double b) { return a < b ? a : b; };
+    auto most = [](double a, double b) { return a > b ? a : b; };
+    const int w16 = waves(out16 ? kMostWaves<true, 1> : kMostWaves<false, 1>), w64 = waves(kMostWaves<true, 4>);
+    // the rows of an expert with four times the mean go to workgroups of their own; one with eight times the mean is reckoned with
+    const double busy = least(M, 4 * r), busiest = least(M, 8 * r);
+    const int d16 = (int)least(8, up(busy / 16)), d64 = (int)least(8, up(busy / 64));
+    const double p16 = most(1.0, r / 16 + 0.5), p64 = most(1.0, r / 64 + 0.4);
+    Choice best = {16, w16, d16};
+    double t = 3 + most(p16 * megabytes / 6.0, up(busiest / 16 / d16) * (1 + 1.6 * up(kb / w16)));
+    auto consider = [&](double time, Choice c) {
+        if (time < t) {
+            t = time;
+            best = c;
+        }
+    };
+    const double pass64 = 1 + (1.6 + 1.6 * least(r, 64) / 64) * up(kb / w64);
+    consider(3 + most(p64 * megabytes / 6.0, most(up(busiest / 64 / d64) * pass64, p64 * pass64 * groups * w64 / cus / 7)), {64, w64, d64});
+    for (int tokens = 128; tokens <= 256 && K > kBlock; tokens *= 2) {   // (the tiles' loads are two steps ahead of them)
+        const double per_expert = up(r / tokens), rounds = up(per_expert * experts * ((N + kTile - 1) / kTile) / cus), full = least(r, tokens) / tokens;
+        const double step = tokens == 128 ? (out16 ? 0.7 + 0.55 * full : 1.15 + 1.25 * full) : (out16 ? 0.9 + 1.15 * full : 2.3 + 1.9 * full);
+        consider(3 + most(megabytes / 5.3, rounds * kb * step), {tokens, 0, 0});
+    }
+    return best;
+}
+
 }  // namespace
 
 }  // namespace moe
@@ -507,33 +559,21 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
     hipError_t err;
     const int cus = device_cus(&err);
     if (err != hipSuccess) return launch_failed(err);
-    const size_t experts = E < M ? E : M;
-    // Which kernel, by the mean number of rows an expert has (64 experts of 2816 x 2048, us; 40 of 2040 x 1000 in brackets):
-    //   rows          6     12    24 (25)    47     94    187    281    768
-    //   streaming    60     80   135 (42)   234      -      -      -      -
-    //   128 tokens   70     70    73 (16)    78     89    134    169    363
-    //   256 tokens   74     75    78 (20)    83     91    119    182    334
-    // Tiles that would leave half of the device idle are left to the streaming kernel, which cuts the work finer.
-    const bool few = M / E < 8;
-    const int tokens = M / E <= 128 ? 128 : 256;
-    const size_t tiles = ((size_t)(M + tokens - 1) / tokens + experts) * ((N + kTile - 1) / kTile);   // (at most)
-    if (tiles >= (size_t)1 << 30) return MOE_ERR_SHAPE;
-    if (!few && K > kBlock && tiles >= (size_t)cus / 2) {
-        const void *fn = tokens == 128 ? (out_bf16 ? (const void *)tile_matmul_kernel<true, 4> : (const void *)tile_matmul_kernel<false, 4>)
-                                       : (out_bf16 ? (const void *)tile_matmul_kernel<true, 8> : (const void *)tile_matmul_kernel<false, 8>);
+    if ((size_t)((M + 127) / 128 + E) * ((N + kTile - 1) / kTile) >= (size_t)1 << 30) return MOE_ERR_SHAPE;
+    const Choice c = choose(M, N, K, E, out_bf16 != 0, cus);
+    if (c.tokens >= 128) {
+        const size_t tiles = ((size_t)(M + c.tokens - 1) / c.tokens + (E < M ? E : M)) * ((N + kTile - 1) / kTile);   // (at most)
+        const void *fn = c.tokens == 128 ? (out_bf16 ? (const void *)tile_matmul_kernel<true, 4> : (const void *)tile_matmul_kernel<false, 4>)
+                                         : (out_bf16 ? (const void *)tile_matmul_kernel<true, 8> : (const void *)tile_matmul_kernel<false, 8>);
         return launch_rows(fn, dim3(tiles < (size_t)cus ? (unsigned)tiles : cus), kTileThreads, &a,
-                           tokens == 128 ? TileSize<4>::kLds : TileSize<8>::kLds, stream, MOE_KERNEL_MATMUL);
+                           c.tokens == 128 ? TileSize<4>::kLds : TileSize<8>::kLds, stream, MOE_KERNEL_MATMUL);
     }
-    // sixteen wavefronts to a CU, as far as the columns go round
-    const size_t groups = experts * ((N + 31) / 32);
-    const int most = few && out_bf16 ? kMostWaves<true, 1> : kMostWaves<false, 1>;
-    int waves = 4;
-    while (waves < most && groups * waves < (size_t)cus * 16 && K / kBlock >= 2 * waves) waves *= 2;
-    const void *fn = few ? (out_bf16 ? (const void *)stream_matmul_kernel<true, 1, 2> : (const void *)stream_matmul_kernel<false, 1, 2>)
-                         : (out_bf16 ? (const void *)stream_matmul_kernel<true, 4, 1> : (const void *)stream_matmul_kernel<false, 4, 1>);
+    const void *fn = c.tokens == 16 ? (out_bf16 ? (const void *)stream_matmul_kernel<true, 1, 2> : (const void *)stream_matmul_kernel<false, 1, 2>)
+                                    : (out_bf16 ? (const void *)stream_matmul_kernel<true, 4, 1> : (const void *)stream_matmul_kernel<false, 4, 1>);
     // Where most experts have no rows, workgroups for the rows: those of an expert without rows only come and go, but thousands of
     // them take longer than the search of the one for a row does (6 rows on 64 experts of 2816 x 2048: 11.6 against 12.2 us; 54 rows
     // 21.9 against 20.0).
     a.by_row = M <= E / 8;
-    return launch_rows(fn, dim3((N + 31) / 32, a.by_row ? M : E), waves * kWave, &a, (size_t)waves * 2 * (few ? 1 : 4) * kWave * 16, stream, MOE_KERNEL_MATMUL);
+    return launch_rows(fn, dim3((N + 31) / 32, a.by_row ? M : E, c.depth), c.waves * kWave, &a, (size_t)c.waves * 2 * (c.tokens / 16) * kWave * 16, stream,
+                       MOE_KERNEL_MATMUL);
 }
