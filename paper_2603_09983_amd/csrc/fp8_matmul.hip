@@ -5,6 +5,7 @@
 // Weight rows are the MFMA's rows and tokens its columns, so that a lane's four results belong to one token and take one scale.
 #include "../../include/moe_spac.h"
 #include "rows_device.h"
+#include <math.h>
 
 namespace moe {
 
@@ -275,6 +276,23 @@ __device__ __forceinline__ void count_tiles(int tokens, const int32_t *offsets, 
     __syncthreads();
 }
 
+// Where tile t lies.  An expert's tiles: its row tiles (TOKENS rows) first, then the next ROWS weight rows.
+struct Place {
+    int e, n0, r0, end;
+};
+template <int ROWS, int TOKENS>
+__device__ __forceinline__ Place place_of(const MatmulArgs &a, const int32_t *first, int tiles_n, int t)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    int e = -1;   // the last expert whose first tile is not behind t
+    for (int i = 0; i < a.E; i += kWave)
+        e += __popcll(__ballot(i + lane < a.E && first[i + lane < a.E ? i + lane : 0] * tiles_n <= t));
+    const int f = __builtin_amdgcn_readfirstlane(first[e]), m = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
+    const int local = t - f * tiles_n, n = local / m;
+    const int lo = clamped(a.offsets[e], a.M), hi = clamped(a.offsets[e + 1], a.M);
+    return Place{e, n * ROWS, lo + (local - n * m) * TOKENS, hi};
+}
+
 template <bool OUT16, int J>
 __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
 {
@@ -286,19 +304,7 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     count_tiles(kTokens, a.offsets, a.M, a.E, first, first + kMaxC + 1);
     const int total = __builtin_amdgcn_readfirstlane(first[a.E]) * tiles_n;
 
-    // Where a tile lies.  An expert's tiles: its row tiles first, then the next 256 weight rows.
-    struct Place {
-        int e, n0, r0, end;
-    };
-    auto place = [&](int t) {
-        int e = -1;   // the last expert whose first tile is not behind t
-        for (int i = 0; i < a.E; i += kWave)
-            e += __popcll(__ballot(i + lane < a.E && first[i + lane < a.E ? i + lane : 0] * tiles_n <= t));
-        const int f = __builtin_amdgcn_readfirstlane(first[e]), m = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
-        const int local = t - f * tiles_n, n = local / m;
-        const int lo = clamped(a.offsets[e], a.M), hi = clamped(a.offsets[e + 1], a.M);
-        return Place{e, n * kTile, lo + (local - n * m) * kTokens, hi};
-    };
+    auto place = [&](int t) { return place_of<kTile, kTokens>(a, first, tiles_n, t); };
 
     // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word each.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
@@ -491,54 +497,245 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way to the LDS of a workgroup that has ended)
 }
 
-// Which kernel takes a call: the one that should be the fastest by what they measured, from the sizes alone (the mean number of rows an
-// expert has, r).  us; 64 experts of 2816 x 2048 where nothing else is said, bf16 results:
-//      r                  6     12     24     47     94    187    281    768     64 (one expert)  12 (8 of 448 x 5664)  364 (8 of 328 x 5176)
-//      streaming, 16     60     82    148    262      -      -      -      -     20                12                     -
-//      streaming, 64     86     92    108    142      -      -      -      -     11                14                     111
-//      tiles of 128      69     70     73     78     89    134    169    363     16                35                     47
-//      tiles of 256      73     75     78     82     91    119    182    334     20                47                     65
-// The streaming kernels: so many passes over an expert's rows, each bound by the weights' bytes (6 TB/s) or by the blocks that a wavefront
-// loads one after the other (1.6 us; as much again for 64 rows that differ, up to seven wavefronts a CU).
-// The tiles: rounds of them over the CUs, each as many steps as there are blocks, a step's time by how many of its rows there are; or
-// the weights' bytes again (5.3 TB/s).
+// ---- the same with smaller tiles: 128 weight rows x 128 tokens, four steps in LDS ----
+// For calls of few tiles, where a step's time is the latency of its loads and of LDS.  Loads are four steps ahead of the products, and a
+// wavefront (64 weight rows x 32 tokens) reads the next step's operands from LDS while it multiplies this one's: behind a step's one
+// barrier the matrix cores have work at once.  A step of 128 columns takes 0.9 us (bf16 results), against 1.3 us of 256 x 128 and 2 us of
+// 256 x 256 (530 tokens' 4 choices of 8 experts of 512 x 7168: 40 against 57 and 85 us); the larger tiles read and move less.
+constexpr int kRing = 4, kRingTile = 128;
+constexpr int kRingHalf = kRingTile * kBlock, kRingStage = 2 * kRingHalf;
+constexpr int kRingChunk = kChunk * (kRingTile + kWave) * 4, kRingScales = kRing * kRingStage;
+constexpr int kRingTable = kRingScales + kRing * kRingChunk, kRingLds = kRingTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
+static_assert(kRingLds <= kLdsBytes, "the steps, their scales, the experts' first tiles");
+
+template <bool OUT16>
+__global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    int32_t *first = (int32_t *)(lds + kRingTable);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock, tiles_n = (a.N + kRingTile - 1) / kRingTile;
+    count_tiles(kRingTile, a.offsets, a.M, a.E, first, first + kMaxC + 1);
+    const int total = __builtin_amdgcn_readfirstlane(first[a.E]) * tiles_n;
+    const int G = gridDim.x, xcds = G % 8 ? 1 : 8, b0 = (blockIdx.x % xcds) * (G / xcds) + blockIdx.x / xcds;
+    if (b0 >= total) return;
+    auto place = [&](int t) { return place_of<kRingTile, kRingTile>(a, first, tiles_n, t); };
+
+    // The loads' walk over the steps of all tiles: two 16-byte words a thread of both operands, rows tid / 8 and 64 further on; the scales
+    // of four blocks at a time, tokens' by wavefronts 0 and 1, the weights' by wavefront 2 (every lane the same).
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+    const int by_word = a.scale_words, s_row = by_word ? kChunk * 4 : 4, s_block = by_word ? 4 : kRingTile * 4, sw_block = by_word ? 4 : kWave * 4;
+    const uint8_t *wbase, *xbase;
+    const float *sbase;
+    uint32_t wat[2], xat[2], sat;
+    int fetched = 0, stage_in = 0, chunk_in = -1;   // blocks of the walk's tile, where the next step goes
+    auto start = [&](const Place &p) {
+        const int row = tid / 8, key = (row & 3) | ((row >> 1) & 4);
+        wbase = a.w + ((size_t)p.e * a.N + p.n0) * a.K;
+        xbase = a.a + (size_t)p.r0 * a.K;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int n = row + 64 * i < a.N - p.n0 ? row + 64 * i : a.N - p.n0 - 1;
+            const int r = row + 64 * i < p.end - p.r0 ? row + 64 * i : p.end - p.r0 - 1;
+            wat[i] = (uint32_t)n * a.K + ((tid & 7) ^ key) * 16;
+            xat[i] = (uint32_t)r * a.K + ((tid & 7) ^ (row & 7)) * 16;
+        }
+        if (w < 2) {
+            sbase = a.a_scale + (size_t)p.r0 * kb;
+            sat = (uint32_t)(tid < p.end - p.r0 ? tid : p.end - p.r0 - 1) * kb * 4;
+        } else {
+            sbase = a.w_scale + ((size_t)p.e * ((a.N + kBlock - 1) / kBlock) + p.n0 / kBlock) * kb;
+            sat = 0;
+        }
+        fetched = 0;
+    };
+    auto fetch = [&]() {
+        if (fetched % kChunk == 0) {
+            chunk_in = (chunk_in + 1) % kRing;
+            if (w < 3) {
+                const uint32_t to = lds0 + kRingScales + chunk_in * kRingChunk + (w < 2 ? w * kWave * s_row : kChunk * kRingTile * 4);
+                if (by_word) {
+                    fetch16(to, sat, sbase + fetched);
+                } else {
+                    for (int i = 0; i < kChunk && fetched + i < kb; ++i) fetch4(to + i * (w < 2 ? s_block : sw_block), sat, sbase + fetched + i);
+                }
+            }
+        }
+        const uint32_t to = lds0 + stage_in * kRingStage + w * 1024;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            fetch16(to + i * 8192, wat[i], wbase);
+            fetch16(to + kRingHalf + i * 8192, xat[i], xbase);
+        }
+        wbase += kBlock;
+        xbase += kBlock;
+        ++fetched;
+        stage_in = (stage_in + 1) % kRing;
+    };
+
+    const int wn = w & 1, wm = w >> 1;
+    const uint32_t wread = (64 * wn + 8 * (col >> 2) + (col & 3)) * kBlock + ((grp ^ (col & 7)) << 4);   // (that row's key: col & 7)
+    const uint32_t xread = kRingHalf + (32 * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
+    const uint32_t sread = (32 * wm + col) * s_row;
+    int stage = 0, chunk = -1;   // of the operands read last
+    struct Step {
+        u32x4 w[4][2], x[2][2];
+        float s[2];
+    };
+    auto read_w = [&](Step &o, int i) {
+        const uint8_t *const q = lds + stage * kRingStage + ((i >> 1) * 32 + (i & 1) * 4) * kBlock;
+        o.w[i][0] = *(const u32x4 *)(q + wread);
+        o.w[i][1] = *(const u32x4 *)(q + (wread ^ 64));
+    };
+    auto read_x = [&](Step &o, int block) {
+        if (block % kChunk == 0) chunk = (chunk + 1) % kRing;
+        const uint8_t *const st = lds + kRingScales + chunk * kRingChunk;
+        const float sw = *(const float *)(st + kChunk * kRingTile * 4 + (block % kChunk) * sw_block);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint8_t *const q = lds + stage * kRingStage + j * 16 * kBlock;
+            o.x[j][0] = *(const u32x4 *)(q + xread);
+            o.x[j][1] = *(const u32x4 *)(q + (xread ^ 64));
+            o.s[j] = *(const float *)(st + (block % kChunk) * s_block + sread + j * 16 * s_row) * sw;
+        }
+    };
+
+    Place now = place(b0), next = now;   // (K has at least four blocks: the walk of the loads is in this tile or the next)
+    start(now);
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) fetch();
+    asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    Step step;
+    read_x(step, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) read_w(step, i);
+    f32x4 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    bool waited = false;   // the next step's loads have been waited for in front of a tile's stores
+    for (int t = b0; t < total; t += G) {
+        if (t + G < total) next = place(t + G);
+        for (int b = 0; b < kb; ++b) {
+            // The next step has arrived here (the loads of the two behind it may be on their way), and this one's operands are in
+            // registers; then everybody's: its place is free.
+            if (waited) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+            waited = false;
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (fetched == kb) start(next);   // (behind the last tile its own steps once more, not used)
+            fetch();
+            stage = (stage + 1) % kRing;
+            Step ahead;
+            read_x(ahead, b + 1 < kb ? b + 1 : 0);
+            const Operand<!OUT16> x0(step.x[0][0], step.x[0][1]), x1(step.x[1][0], step.x[1][1]);
+            f32x4 sum[2][2];
+#pragma unroll
+            for (int i = 0; i <= 4; ++i) {
+                if (i < 4) {
+                    const Operand<!OUT16> y(step.w[i][0], step.w[i][1]);
+                    sum[i & 1][0] = mfma128(y, x0);
+                    sum[i & 1][1] = mfma128(y, x1);
+                    read_w(ahead, i);
+                }
+                if (i > 0) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) acc[i - 1][j][c] = __builtin_fmaf(sum[~i & 1][j][c], step.s[j], acc[i - 1][j][c]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            step = ahead;
+        }
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        waited = true;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = now.r0 + 32 * wm + 16 * j + col;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int n = now.n0 + 64 * wn + 32 * i + 8 * grp;
+                const f32x4 u = acc[2 * i][j], v = acc[2 * i + 1][j];
+                if (r < now.end && n < a.N) {
+                    if (OUT16) {
+                        const u32x4 o = {pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                        *(u32x4 *)((uint16_t *)a.out + (size_t)r * a.N + n) = o;
+                    } else {
+                        f32x4 *o = (f32x4 *)((float *)a.out + (size_t)r * a.N + n);
+                        o[0] = u;
+                        o[1] = v;
+                    }
+                }
+                acc[2 * i][j] = acc[2 * i + 1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        now = next;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way to the LDS of a workgroup that has ended)
+}
+
+// Which kernel takes a call: the one that should be the fastest by what they measured, from the sizes alone.  us, bf16 results / fp32; r:
+// rows an expert, evenly.  64 experts of 2816 x 2048, then one of them, then 8 of 512 x 7168:
+//                 r = 6     12       24       47       94       187      281      768         64      512        12       265
+//      16 rows     62/68   79/84   147/153  256/264  493/505  955/981   1434/-      -       12/13      -       16/15   127/124
+//      64 rows     84/100  93/107  109/124  143/154  279/298  508/540  752/797      -       11/12      -       18/19    77/79
+//      128 x 128   74/120  76/120   78/122   83/125   93/132  142/243  208/353  430/719     14/23    16/25     37/64    40/67
+//      256 x 128   70/75   71/78    74/83    78/90    90/124  142/220  178/288  357/623     16/25    22/37     43/69    57/105
+//      256 x 256   73/126  74/126   77/130   82/135   91/144  117/216  192/388  332/658     20/42    31/66     56/128   85/201
+// (16 and 64 rows: the streaming kernels; the others: tiles of weight rows x rows.)  Over 3000 calls of random sizes the choice took 1.03
+// times the fastest's time, in one call of thirty more than 1.3 times; without one of the kernels the fastest took 1.006 (256 x 256) to
+// 1.06 (16 rows) times as long as with all.
+//
+// All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernels: what a CU
+// takes in, weights and rows, at 35 B/ns; or the blocks that a wavefront loads one after the other (1.1 us; as much again for 64 rows that
+// differ) in each pass over a busy expert's rows.  The tiles: rounds of them over the CUs, each as many steps as there are blocks, a
+// step's time by how many of its rows there are.
 struct Choice {
-    int tokens;          // 16, 64: the streaming kernel; 128, 256: tiles
-    int waves, depth;    // the streaming kernel's wavefronts, and workgroups to an expert's rows
+    enum { kStream16, kStream64, kTiles128, kTiles256x128, kTiles256 } kernel;
+    int waves, depth;    // the streaming kernels' wavefronts, and workgroups to an expert's rows
 };
 
 Choice choose(int M, int N, int K, int E, bool out16, int cus)
 {
-    const double kb = K / kBlock, experts = E < M ? E : M, r = M / experts, groups = experts * ((N + 31) / 32);
-    const double megabytes = experts * N * K * 1e-6;
-    auto waves = [&](int most) {   // sixteen to a CU, as far as the columns go round
-        int w = 4;
-        while (w < most && groups * w < cus * 16.0 && kb >= 2 * w) w *= 2;
-        return w;
-    };
     auto up = [](double x) { return (double)(long long)(x + 0.999999); };
     auto least = [](double a, double b) { return a < b ? a : b; };
     auto most = [](double a, double b) { return a > b ? a : b; };
-    const int w16 = waves(out16 ? kMostWaves<true, 1> : kMostWaves<false, 1>), w64 = waves(kMostWaves<true, 4>);
-    // the rows of an expert with four times the mean go to workgroups of their own; one with eight times the mean is reckoned with
+    const double kb = up((double)K / kBlock);
+    const double experts = E * (1 - exp(-(double)M / E));   // that have rows, where each row is anybody's
+    const double r = M / experts, groups = experts * ((N + 31) / 32), megabytes = experts * N * K * 1e-6;
+    // an expert with four times the mean has workgroups for all its rows; one with eight times the mean is reckoned with
     const double busy = least(M, 4 * r), busiest = least(M, 8 * r);
-    const int d16 = (int)least(8, up(busy / 16)), d64 = (int)least(8, up(busy / 64));
-    const double p16 = most(1.0, r / 16 + 0.5), p64 = most(1.0, r / 64 + 0.4);
-    Choice best = {16, w16, d16};
-    double t = 3 + most(p16 * megabytes / 6.0, up(busiest / 16 / d16) * (1 + 1.6 * up(kb / w16)));
+    Choice best = {};
+    double least_time = 1e30;
     auto consider = [&](double time, Choice c) {
-        if (time < t) {
-            t = time;
+        if (time < least_time) {
+            least_time = time;
             best = c;
         }
     };
-    const double pass64 = 1 + (1.6 + 1.6 * least(r, 64) / 64) * up(kb / w64);
-    consider(3 + most(p64 * megabytes / 6.0, most(up(busiest / 64 / d64) * pass64, p64 * pass64 * groups * w64 / cus / 7)), {64, w64, d64});
-    for (int tokens = 128; tokens <= 256 && K > kBlock; tokens *= 2) {   // (the tiles' loads are two steps ahead of them)
-        const double per_expert = up(r / tokens), rounds = up(per_expert * experts * ((N + kTile - 1) / kTile) / cus), full = least(r, tokens) / tokens;
-        const double step = tokens == 128 ? (out16 ? 0.7 + 0.55 * full : 1.15 + 1.25 * full) : (out16 ? 0.9 + 1.15 * full : 2.3 + 1.9 * full);
-        consider(3 + most(megabytes / 5.3, rounds * kb * step), {tokens, 0, 0});
+    for (int tokens = 16; tokens <= 64; tokens *= 4) {
+        int w = 4;   // wavefronts: sixteen to a CU, as far as the columns go round
+        const int w_most = tokens == 64 || !out16 ? 8 : 16;
+        while (w < w_most && groups * w < cus * 16.0 && kb >= 2 * w) w *= 2;
+        const double depth = least(8, up(busy / tokens)), full = least(r, 64) / 64;
+        const double passes = most(1.0, r / tokens + (tokens == 16 ? 0.6 : 0.4));
+        const double taken = 32.0 * K * (tokens == 16 ? 1.4 : 2.4 + 1.3 * full) / 35e3 + w / 16.0;
+        const double block = tokens == 16 ? 1.1 : 1.1 + full;
+        const double time = most(up(groups * passes / cus) * taken * (out16 ? 1.0 : 1.25), up(busiest / tokens / depth) * (0.7 + block * up(kb / w)));
+        consider(1.4 + most(passes * megabytes / 6.7, time), {tokens == 16 ? Choice::kStream16 : Choice::kStream64, w, (int)depth});
     }
+    auto tiles = [&](int rows, int tokens, double step, double rate, Choice c) {
+        const double rounds = up(up(r / tokens) * experts * ((N + rows - 1) / rows) / cus);
+        consider(3.9 + most(megabytes / rate, rounds * kb * step), c);
+    };
+    // (the tiles' loads are four and two steps ahead of them)
+    const double half = least(r, 128) / 128, full = least(r, 256) / 256;
+    if (kb >= 4) tiles(128, 128, out16 ? 0.8 + 0.2 * half : 1.3, out16 ? 4.8 : 4.1, {Choice::kTiles128, 0, 0});
+    if (kb >= 2) tiles(256, 128, out16 ? 0.8 + 0.58 * half : 1.3 + 0.75 * half, out16 ? 5.6 : 4.0, {Choice::kTiles256x128, 0, 0});
+    if (kb >= 2) tiles(256, 256, out16 ? 1.0 + 1.1 * full : 2.8 + 2.3 * full, out16 ? 4.9 : 2.6, {Choice::kTiles256, 0, 0});
     return best;
 }
 
@@ -559,21 +756,28 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
     hipError_t err;
     const int cus = device_cus(&err);
     if (err != hipSuccess) return launch_failed(err);
-    if ((size_t)((M + 127) / 128 + E) * ((N + kTile - 1) / kTile) >= (size_t)1 << 30) return MOE_ERR_SHAPE;
+    if ((size_t)((M + 127) / 128 + E) * ((N + 127) / 128) >= (size_t)1 << 30) return MOE_ERR_SHAPE;
     const Choice c = choose(M, N, K, E, out_bf16 != 0, cus);
-    if (c.tokens >= 128) {
-        const size_t tiles = ((size_t)(M + c.tokens - 1) / c.tokens + (E < M ? E : M)) * ((N + kTile - 1) / kTile);   // (at most)
-        const void *fn = c.tokens == 128 ? (out_bf16 ? (const void *)tile_matmul_kernel<true, 4> : (const void *)tile_matmul_kernel<false, 4>)
-                                         : (out_bf16 ? (const void *)tile_matmul_kernel<true, 8> : (const void *)tile_matmul_kernel<false, 8>);
-        return launch_rows(fn, dim3(tiles < (size_t)cus ? (unsigned)tiles : cus), kTileThreads, &a,
-                           c.tokens == 128 ? TileSize<4>::kLds : TileSize<8>::kLds, stream, MOE_KERNEL_MATMUL);
+    auto tiles = [&](const void *fn, int rows, int tokens, int lds) {
+        const size_t n = ((size_t)(M + tokens - 1) / tokens + (E < M ? E : M)) * ((N + rows - 1) / rows);   // (at most)
+        return launch_rows(fn, dim3(n < (size_t)cus ? (unsigned)n : cus), kTileThreads, &a, lds, stream, MOE_KERNEL_MATMUL);
+    };
+    switch (c.kernel) {
+    case Choice::kTiles128:
+        return tiles(out_bf16 ? (const void *)ring_matmul_kernel<true> : (const void *)ring_matmul_kernel<false>, 128, 128, kRingLds);
+    case Choice::kTiles256x128:
+        return tiles(out_bf16 ? (const void *)tile_matmul_kernel<true, 4> : (const void *)tile_matmul_kernel<false, 4>, 256, 128, TileSize<4>::kLds);
+    case Choice::kTiles256:
+        return tiles(out_bf16 ? (const void *)tile_matmul_kernel<true, 8> : (const void *)tile_matmul_kernel<false, 8>, 256, 256, TileSize<8>::kLds);
+    default: break;
     }
-    const void *fn = c.tokens == 16 ? (out_bf16 ? (const void *)stream_matmul_kernel<true, 1, 2> : (const void *)stream_matmul_kernel<false, 1, 2>)
-                                    : (out_bf16 ? (const void *)stream_matmul_kernel<true, 4, 1> : (const void *)stream_matmul_kernel<false, 4, 1>);
+    const int tokens = c.kernel == Choice::kStream16 ? 16 : 64;
+    const void *fn = tokens == 16 ? (out_bf16 ? (const void *)stream_matmul_kernel<true, 1, 2> : (const void *)stream_matmul_kernel<false, 1, 2>)
+                                  : (out_bf16 ? (const void *)stream_matmul_kernel<true, 4, 1> : (const void *)stream_matmul_kernel<false, 4, 1>);
     // Where most experts have no rows, workgroups for the rows: those of an expert without rows only come and go, but thousands of
     // them take longer than the search of the one for a row does (6 rows on 64 experts of 2816 x 2048: 11.6 against 12.2 us; 54 rows
     // 21.9 against 20.0).
     a.by_row = M <= E / 8;
-    return launch_rows(fn, dim3((N + 31) / 32, a.by_row ? M : E, c.depth), c.waves * kWave, &a, (size_t)c.waves * 2 * (c.tokens / 16) * kWave * 16, stream,
+    return launch_rows(fn, dim3((N + 31) / 32, a.by_row ? M : E, c.depth), c.waves * kWave, &a, (size_t)c.waves * 2 * (tokens / 16) * kWave * 16, stream,
                        MOE_KERNEL_MATMUL);
 }
