@@ -404,71 +404,68 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
             if (b == 0 && t + G < total) next = place(t + G);
             if (b + 2 == kb) start_w(next);
             const uint8_t *const tile = lds + stage * kStageBytes;
-            // (fp32 results of 256 tokens: the weights' wider operands in two passes, so that all stays in registers)
-            constexpr int P = OUT16 || J == 4 ? 1 : 2, I = 4 / P;
-#pragma unroll
-            for (int pass = 0; pass < P; ++pass) {
-                // The loads go out one at a time between the products: the loads of all wavefronts at once keep the address unit busy
-                // for a thousand cycles, in which a wavefront whose turn has not come issues nothing else.  The next step's rows first;
-                // then, when everybody has its weights (the products that read them are on their way), those of the step after next.
-                auto request = [&](int j) {
-                    if (pass == 0 && j < J / 2) fetch_x(stage ^ 1, j);
-                    if (pass == P - 1 && j >= J / 2) {
-                        if (j == J / 2) {
-                            __builtin_amdgcn_s_barrier();
-                            asm volatile("" ::: "memory");
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8 / J; ++i) fetch_w(stage, (j - J / 2) * (8 / J) + i);
-                    }
-                };
-                if (!mine) {
-#pragma unroll
-                    for (int j = 0; j < J; ++j) request(j);
-                    continue;
-                }
-                u32x4 xraw[2], wraw[I][2];
-                auto read_x = [&](int j) {
-                    xraw[0] = *(const u32x4 *)(tile + xread + j * 16 * kBlock);
-                    xraw[1] = *(const u32x4 *)(tile + (xread ^ 64) + j * 16 * kBlock);
-                };
-                read_x(0);
-#pragma unroll
-                for (int i = 0; i < I; ++i) {
-                    const int at = ((pass * I + i) >> 1) * 32 + ((pass * I + i) & 1) * 4;
-                    wraw[i][0] = *(const u32x4 *)(tile + wread + at * kBlock);
-                    wraw[i][1] = *(const u32x4 *)(tile + (wread ^ 64) + at * kBlock);
-                }
-                auto scale = [&](int j) { return *(const float *)(st + sread + j * 16 * s_row); };
-                const float sw = *(const float *)(swt + (wn >> 1) * s_row);
-                Operand<!OUT16> wv[I];
-#pragma unroll
-                for (int i = 0; i < I; ++i) wv[i] = Operand<!OUT16>(wraw[i][0], wraw[i][1]);
-                // sixteen tokens' products while those before are scaled and added (in this order: left to itself the compiler puts
-                // every product's multiply-adds right behind it and waits)
-                f32x4 sum[2][I];
-                float s[2] = {scale(0) * sw, 0.f};
-#pragma unroll
-                for (int j = 0; j <= J; ++j) {
-                    if (j < J) request(j);
-                    const Operand<!OUT16> now(xraw[0], xraw[1]);
-                    float next_scale;
-                    if (j < J - 1) {
-                        read_x(j + 1);
-                        next_scale = scale(j + 1);
+            // The loads go out one at a time between the products: the loads of all wavefronts at once keep the address unit busy
+            // for a thousand cycles, in which a wavefront whose turn has not come issues nothing else.  The next step's rows first;
+            // then, when everybody has its weights (the products that read them are on their way), those of the step after next.
+            auto request = [&](int j) {
+                if (j < J / 2) {
+                    fetch_x(stage ^ 1, j);
+                } else {
+                    if (j == J / 2) {
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
                     }
 #pragma unroll
-                    for (int i = 0; i < I; ++i) {
-                        if (j < J) sum[j & 1][i] = mfma128(wv[i], now);
-                        if (j > 0) {
-#pragma unroll
-                            for (int c = 0; c < 4; ++c)
-                                acc[pass * I + i][j - 1][c] = __builtin_fmaf(sum[~j & 1][i][c], s[~j & 1], acc[pass * I + i][j - 1][c]);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-                    if (j < J - 1) s[~j & 1] = next_scale * sw;
+                    for (int i = 0; i < 8 / J; ++i) fetch_w(stage, (j - J / 2) * (8 / J) + i);
                 }
+            };
+            if (!mine) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) request(j);
+                stage ^= 1;
+                continue;
+            }
+            u32x4 xraw[2], wraw[4][2];
+            auto read_x = [&](int j) {
+                xraw[0] = *(const u32x4 *)(tile + xread + j * 16 * kBlock);
+                xraw[1] = *(const u32x4 *)(tile + (xread ^ 64) + j * 16 * kBlock);
+            };
+            read_x(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = (i >> 1) * 32 + (i & 1) * 4;
+                wraw[i][0] = *(const u32x4 *)(tile + wread + at * kBlock);
+                wraw[i][1] = *(const u32x4 *)(tile + (wread ^ 64) + at * kBlock);
+            }
+            auto scale = [&](int j) { return *(const float *)(st + sread + j * 16 * s_row); };
+            const float sw = *(const float *)(swt + (wn >> 1) * s_row);
+            Operand<!OUT16> wv[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) wv[i] = Operand<!OUT16>(wraw[i][0], wraw[i][1]);
+            // sixteen tokens' products while those before are scaled and added (in this order: left to itself the compiler puts
+            // every product's multiply-adds right behind it and waits)
+            f32x4 sum[2][4];
+            float s[2] = {scale(0) * sw, 0.f};
+#pragma unroll
+            for (int j = 0; j <= J; ++j) {
+                if (j < J) request(j);
+                const Operand<!OUT16> now(xraw[0], xraw[1]);
+                float next_scale;
+                if (j < J - 1) {
+                    read_x(j + 1);
+                    next_scale = scale(j + 1);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (j < J) sum[j & 1][i] = mfma128(wv[i], now);
+                    if (j > 0) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            acc[i][j - 1][c] = __builtin_fmaf(sum[~j & 1][i][c], s[~j & 1], acc[i][j - 1][c]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (j < J - 1) s[~j & 1] = next_scale * sw;
             }
             stage ^= 1;
         }
@@ -684,10 +681,11 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
 //      64 rows     84/100  93/107  109/124  143/154  279/298  508/540  752/797      -       11/12      -       18/19    77/79
 //      128 x 128   74/120  76/120   78/122   83/125   93/132  142/243  208/353  430/719     14/23    16/25     37/64    40/67
 //      256 x 128   70/75   71/78    74/83    78/90    90/124  142/220  178/288  357/623     16/25    22/37     43/69    57/105
-//      256 x 256   73/126  74/126   77/130   82/135   91/144  117/216  192/388  332/658     20/42    31/66     56/128   85/201
+//      256 x 256   73/-    74/-     77/-     82/-     91/-    117/-    192/-    332/-       20/-     31/-      56/-     85/-
 // (16 and 64 rows: the streaming kernels; the others: tiles of weight rows x rows.)  Over 3000 calls of random sizes the choice took 1.03
 // times the fastest's time, in one call of thirty more than 1.3 times; without one of the kernels the fastest took 1.006 (256 x 256) to
-// 1.06 (16 rows) times as long as with all.
+// 1.06 (16 rows) times as long as with all.  (256 x 256 with fp32 results, whose operands are wider than its registers hold at once, was
+// never the fastest by more than 5 %: 126/658 us at 6 and 768 rows.)
 //
 // All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernels: what a CU
 // takes in, weights and rows, at 35 B/ns; or the blocks that a wavefront loads one after the other (1.1 us; as much again for 64 rows that
@@ -703,7 +701,7 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
     auto up = [](double x) { return (double)(long long)(x + 0.999999); };
     auto least = [](double a, double b) { return a < b ? a : b; };
     auto most = [](double a, double b) { return a > b ? a : b; };
-    const double kb = up((double)K / kBlock);
+    const double kb = K / kBlock;
     const double experts = E * (1 - exp(-(double)M / E));   // that have rows, where each row is anybody's
     const double r = M / experts, groups = experts * ((N + 31) / 32), megabytes = experts * N * K * 1e-6;
     // an expert with four times the mean has workgroups for all its rows; one with eight times the mean is reckoned with
@@ -735,7 +733,7 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
     const double half = least(r, 128) / 128, full = least(r, 256) / 256;
     if (kb >= 4) tiles(128, 128, out16 ? 0.8 + 0.2 * half : 1.3, out16 ? 4.8 : 4.1, {Choice::kTiles128, 0, 0});
     if (kb >= 2) tiles(256, 128, out16 ? 0.8 + 0.58 * half : 1.3 + 0.75 * half, out16 ? 5.6 : 4.0, {Choice::kTiles256x128, 0, 0});
-    if (kb >= 2) tiles(256, 256, out16 ? 1.0 + 1.1 * full : 2.8 + 2.3 * full, out16 ? 4.9 : 2.6, {Choice::kTiles256, 0, 0});
+    if (kb >= 2 && out16) tiles(256, 256, 1.0 + 1.1 * full, 4.9, {Choice::kTiles256, 0, 0});
     return best;
 }
 
@@ -768,7 +766,7 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
     case Choice::kTiles256x128:
         return tiles(out_bf16 ? (const void *)tile_matmul_kernel<true, 4> : (const void *)tile_matmul_kernel<false, 4>, 256, 128, TileSize<4>::kLds);
     case Choice::kTiles256:
-        return tiles(out_bf16 ? (const void *)tile_matmul_kernel<true, 8> : (const void *)tile_matmul_kernel<false, 8>, 256, 256, TileSize<8>::kLds);
+        return tiles((const void *)tile_matmul_kernel<true, 8>, 256, 256, TileSize<8>::kLds);
     default: break;
     }
     const int tokens = c.kernel == Choice::kStream16 ? 16 : 64;

@@ -181,6 +181,17 @@ def test_product_many_rows(counts, N, K, dtype):
     _check(*_operands(counts, N, K, 12), dtype)
 
 
+# rows enough for tiles, but few of them; more than one to a workgroup, whose steps are fewer than, as many as and more than are ahead
+FEW = [([600, 5, 900], 1000, 512), ([700, 0, 1300], 520, 1408), ([700, 0, 1300], 136, 5120), ([700, 0, 1300], 4104, 512),
+       ([1, 129, 128, 127, 0, 256] * 3, 1160, 1024), ([40] * 30, 2056, 512), ([19 * i % 61 for i in range(60)], 1032, 640)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("counts,N,K", FEW, ids=[f"{sum(c)}in{len(c)}x{n}x{k}" for c, n, k in FEW])
+def test_product_few_tiles(counts, N, K, dtype):
+    _check(*_operands(counts, N, K, 14, lead=2, tail=3), dtype)
+
+
 def test_many_rows_rows_of_no_expert_and_nan():
     a, sa, w, sw, offsets = _operands([300, 0, 700], 4104, 512, 13, lead=5, tail=30)
     _check(a, sa, w, sw, offsets, torch.bfloat16)
