@@ -496,9 +496,11 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
 
 // ---- the same with smaller tiles: 128 weight rows x 128 tokens, four steps in LDS ----
 // For calls of few tiles, where a step's time is the latency of its loads and of LDS.  Loads are four steps ahead of the products, and a
-// wavefront (64 weight rows x 32 tokens) reads the next step's operands from LDS while it multiplies this one's: behind a step's one
-// barrier the matrix cores have work at once.  A step of 128 columns takes 0.9 us (bf16 results), against 1.3 us of 256 x 128 and 2 us of
-// 256 x 256 (530 tokens' 4 choices of 8 experts of 512 x 7168: 40 against 57 and 85 us); the larger tiles read and move less.
+// wavefront (32 weight rows x 64 tokens) reads the next step's operands from LDS while it multiplies this one's: behind a step's one
+// barrier the matrix cores have work at once; the halves of 32 tokens that are not there are left out.  A step of 128 columns takes 0.7 us
+// (bf16 results; 0.5 with up to 32 tokens), against 1.2 us of 256 x 128 and 1.7 us of 256 x 256 (2120 rows of 8 experts of 512 x 7168:
+// 40 against 57 and 84 us); the larger tiles read and move less.  Wavefronts of 64 weight rows x 32 tokens: up to 32 tokens 20 % slower,
+// fp32 results of full tiles 5 % faster.
 constexpr int kRing = 4, kRingTile = 128;
 constexpr int kRingHalf = kRingTile * kBlock, kRingStage = 2 * kRingHalf;
 constexpr int kRingChunk = kChunk * (kRingTile + kWave) * 4, kRingScales = kRing * kRingStage;
@@ -570,31 +572,33 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
         stage_in = (stage_in + 1) % kRing;
     };
 
-    const int wn = w & 1, wm = w >> 1;
-    const uint32_t wread = (64 * wn + 8 * (col >> 2) + (col & 3)) * kBlock + ((grp ^ (col & 7)) << 4);   // (that row's key: col & 7)
-    const uint32_t xread = kRingHalf + (32 * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
-    const uint32_t sread = (32 * wm + col) * s_row;
-    int stage = 0, chunk = -1;   // of the operands read last
+    const int wn = w & 3, wm = w >> 2;
+    const uint32_t wread = (32 * wn + 8 * (col >> 2) + (col & 3)) * kBlock + ((grp ^ (col & 7)) << 4);   // (that row's key: col & 7)
+    const uint32_t xread = kRingHalf + (64 * wm + col) * kBlock + ((grp ^ (col & 7)) << 4);
+    const uint32_t sread = (64 * wm + col) * s_row;
+    int stage = 0, chunk = 0;   // of the operands read last
     struct Step {
-        u32x4 w[4][2], x[2][2];
-        float s[2];
+        u32x4 w[2][2], x[4][2];
+        float s[4];
     };
-    auto read_w = [&](Step &o, int i) {
-        const uint8_t *const q = lds + stage * kRingStage + ((i >> 1) * 32 + (i & 1) * 4) * kBlock;
-        o.w[i][0] = *(const u32x4 *)(q + wread);
-        o.w[i][1] = *(const u32x4 *)(q + (wread ^ 64));
+    auto read = [&](u32x4 *o, uint32_t at) {
+        o[0] = *(const u32x4 *)(lds + stage * kRingStage + at);
+        o[1] = *(const u32x4 *)(lds + stage * kRingStage + (at ^ 64));
     };
-    auto read_x = [&](Step &o, int block) {
-        if (block % kChunk == 0) chunk = (chunk + 1) % kRing;
+    auto read_w = [&](Step &o) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) read(o.w[i], wread + i * 4 * kBlock);
+    };
+    auto read_x = [&](Step &o, int j, int block) {
         const uint8_t *const st = lds + kRingScales + chunk * kRingChunk;
         const float sw = *(const float *)(st + kChunk * kRingTile * 4 + (block % kChunk) * sw_block);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const uint8_t *const q = lds + stage * kRingStage + j * 16 * kBlock;
-            o.x[j][0] = *(const u32x4 *)(q + xread);
-            o.x[j][1] = *(const u32x4 *)(q + (xread ^ 64));
-            o.s[j] = *(const float *)(st + (block % kChunk) * s_block + sread + j * 16 * s_row) * sw;
-        }
+        read(o.x[j], xread + j * 16 * kBlock);
+        o.s[j] = *(const float *)(st + (block % kChunk) * s_block + sread + j * 16 * s_row) * sw;
+    };
+    // How many of a wavefront's two halves of 32 tokens there are in a tile; without any it only loads.
+    auto halves = [&](const Place &p) {
+        const int rows = p.end - p.r0 - 64 * wm;
+        return p.n0 + 32 * wn >= a.N || rows <= 0 ? 0 : rows <= 32 ? 1 : 2;
     };
 
     Place now = place(b0), next = now;   // (K has at least four blocks: the walk of the loads is in this tile or the next)
@@ -605,15 +609,17 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     Step step;
-    read_x(step, 0);
+    read_w(step);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) read_w(step, i);
-    f32x4 acc[4][2];
+    for (int j = 0; j < 4; ++j) read_x(step, j, 0);
+    int work = halves(now), next_work = work;
+    f32x4 acc[2][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i][0] = acc[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 4; ++j) acc[0][j] = acc[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     bool waited = false;   // the next step's loads have been waited for in front of a tile's stores
     for (int t = b0; t < total; t += G) {
         if (t + G < total) next = place(t + G);
+        next_work = halves(next);
         for (int b = 0; b < kb; ++b) {
             // The next step has arrived here (the loads of the two behind it may be on their way), and this one's operands are in
             // registers; then everybody's: its place is free.
@@ -625,70 +631,81 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
             if (fetched == kb) start(next);   // (behind the last tile its own steps once more, not used)
             fetch();
             stage = (stage + 1) % kRing;
+            const int after = b + 1 < kb ? b + 1 : 0;
+            if (after % kChunk == 0) chunk = (chunk + 1) % kRing;
+            const int most = after == 0 && next_work > work ? next_work : work;   // (for this step's products and the next one's operands)
+            if (most == 0) continue;
             Step ahead;
-            read_x(ahead, b + 1 < kb ? b + 1 : 0);
-            const Operand<!OUT16> x0(step.x[0][0], step.x[0][1]), x1(step.x[1][0], step.x[1][1]);
+            read_w(ahead);
+            const Operand<!OUT16> y0(step.w[0][0], step.w[0][1]), y1(step.w[1][0], step.w[1][1]);
             f32x4 sum[2][2];
+            auto multiply = [&](int j) {
+                const Operand<!OUT16> x(step.x[j][0], step.x[j][1]);
+                sum[j & 1][0] = mfma128(y0, x);
+                sum[j & 1][1] = mfma128(y1, x);
+                read_x(ahead, j, after);
+            };
+            auto add = [&](int j) {
 #pragma unroll
-            for (int i = 0; i <= 4; ++i) {
-                if (i < 4) {
-                    const Operand<!OUT16> y(step.w[i][0], step.w[i][1]);
-                    sum[i & 1][0] = mfma128(y, x0);
-                    sum[i & 1][1] = mfma128(y, x1);
-                    read_w(ahead, i);
-                }
-                if (i > 0) {
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) acc[i - 1][j][c] = __builtin_fmaf(sum[~i & 1][j][c], step.s[j], acc[i - 1][j][c]);
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int c = 0; c < 4; ++c) acc[i][j][c] = __builtin_fmaf(sum[j & 1][i][c], step.s[j], acc[i][j][c]);
+                if (OUT16) __builtin_amdgcn_sched_barrier(0);   // (fp32 results are 4 % faster in the compiler's order)
+            };
+            multiply(0);
+            if (OUT16) __builtin_amdgcn_sched_barrier(0);
+            multiply(1);
+            add(0);
+            if (most == 2) {
+                multiply(2);
+                add(1);
+                multiply(3);
+                add(2);
+                add(3);
+            } else {
+                add(1);
             }
             step = ahead;
         }
         asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
         waited = true;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int r = now.r0 + 32 * wm + 16 * j + col;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int n = now.n0 + 64 * wn + 32 * i + 8 * grp;
-                const f32x4 u = acc[2 * i][j], v = acc[2 * i + 1][j];
-                if (r < now.end && n < a.N) {
-                    if (OUT16) {
-                        const u32x4 o = {pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-                        *(u32x4 *)((uint16_t *)a.out + (size_t)r * a.N + n) = o;
-                    } else {
-                        f32x4 *o = (f32x4 *)((float *)a.out + (size_t)r * a.N + n);
-                        o[0] = u;
-                        o[1] = v;
-                    }
+        for (int j = 0; j < 4; ++j) {
+            const int r = now.r0 + 64 * wm + 16 * j + col, n = now.n0 + 32 * wn + 8 * grp;
+            const f32x4 u = acc[0][j], v = acc[1][j];
+            if (r < now.end && n < a.N) {
+                if (OUT16) {
+                    const u32x4 o = {pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]), pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+                    *(u32x4 *)((uint16_t *)a.out + (size_t)r * a.N + n) = o;
+                } else {
+                    f32x4 *o = (f32x4 *)((float *)a.out + (size_t)r * a.N + n);
+                    o[0] = u;
+                    o[1] = v;
                 }
-                acc[2 * i][j] = acc[2 * i + 1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
+            acc[0][j] = acc[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         now = next;
+        work = next_work;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is on its way to the LDS of a workgroup that has ended)
 }
 
 // Which kernel takes a call: the one that should be the fastest by what they measured, from the sizes alone.  us, bf16 results / fp32; r:
 // rows an expert, evenly.  64 experts of 2816 x 2048, then one of them, then 8 of 512 x 7168:
-//                 r = 6     12       24       47       94       187      281      768         64      512        12       265
-//      16 rows     62/68   79/84   147/153  256/264  493/505  955/981   1434/-      -       12/13      -       16/15   127/124
-//      64 rows     84/100  93/107  109/124  143/154  279/298  508/540  752/797      -       11/12      -       18/19    77/79
-//      128 x 128   74/120  76/120   78/122   83/125   93/132  142/243  208/353  430/719     14/23    16/25     37/64    40/67
-//      256 x 128   70/75   71/78    74/83    78/90    90/124  142/220  178/288  357/623     16/25    22/37     43/69    57/105
-//      256 x 256   73/-    74/-     77/-     82/-     91/-    117/-    192/-    332/-       20/-     31/-      56/-     85/-
-// (16 and 64 rows: the streaming kernels; the others: tiles of weight rows x rows.)  Over 3000 calls of random sizes the choice took 1.03
-// times the fastest's time, in one call of thirty more than 1.3 times; without one of the kernels the fastest took 1.006 (256 x 256) to
-// 1.06 (16 rows) times as long as with all.  (256 x 256 with fp32 results, whose operands are wider than its registers hold at once, was
-// never the fastest by more than 5 %: 126/658 us at 6 and 768 rows.)
+//            r = 6         12        24        47        94        187       281       768          64        512       12        265
+//      16 rows   62/67     77/83     145/152   254/262   491/507   955/975   1433/-    -            12/13     -         16/15     126/122
+//      64 rows   86/99     91/108    108/123   142/153   277/297   506/539   748/792   -            12/12     -         18/19     76/78
+//      128 x 128 70/72     72/75     74/81     81/92     92/129    144/241   195/327   434/737      13/18     16/26     25/34     40/69
+//      256 x 128 69/74     70/77     74/81     78/89     89/120    142/213   176/278   358/610      16/25     22/37     43/68     57/104
+//      256 x 256 72/-      73/-      76/-      80/-      90/-      114/-     187/-     322/-        20/-      31/-      55/-      84/-
+// (16 and 64 rows: the streaming kernels; the others: tiles of weight rows x rows.  256 x 256 with fp32 results, whose operands are wider
+// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3800 calls of random sizes the choice took 1.035 times
+// the fastest's time, 1.055 where the routing was skewed, which it does not see; without one of the kernels the fastest took 1.006
+// (256 x 256) to 1.04 (16 rows, 128 x 128) times as long as with all.
 //
 // All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernels: what a CU
-// takes in, weights and rows, at 35 B/ns; or the blocks that a wavefront loads one after the other (1.1 us; as much again for 64 rows that
+// takes in, weights and rows, at 35 B/ns; or the blocks that a wavefront loads one after the other (0.9 us, 1.5 for 64 rows that
 // differ) in each pass over a busy expert's rows.  The tiles: rounds of them over the CUs, each as many steps as there are blocks, a
 // step's time by how many of its rows there are.
 struct Choice {
@@ -704,8 +721,8 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
     const double kb = K / kBlock;
     const double experts = E * (1 - exp(-(double)M / E));   // that have rows, where each row is anybody's
     const double r = M / experts, groups = experts * ((N + 31) / 32), megabytes = experts * N * K * 1e-6;
-    // an expert with four times the mean has workgroups for all its rows; one with eight times the mean is reckoned with
-    const double busy = least(M, 4 * r), busiest = least(M, 8 * r);
+    // an expert with four times the mean has workgroups for all its rows; one with six times the mean is reckoned with
+    const double busy = least(M, 4 * r), busiest = least(M, 6 * r);
     Choice best = {};
     double least_time = 1e30;
     auto consider = [&](double time, Choice c) {
@@ -719,11 +736,11 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
         const int w_most = tokens == 64 || !out16 ? 8 : 16;
         while (w < w_most && groups * w < cus * 16.0 && kb >= 2 * w) w *= 2;
         const double depth = least(8, up(busy / tokens)), full = least(r, 64) / 64;
-        const double passes = most(1.0, r / tokens + (tokens == 16 ? 0.6 : 0.4));
-        const double taken = 32.0 * K * (tokens == 16 ? 1.4 : 2.4 + 1.3 * full) / 35e3 + w / 16.0;
-        const double block = tokens == 16 ? 1.1 : 1.1 + full;
-        const double time = most(up(groups * passes / cus) * taken * (out16 ? 1.0 : 1.25), up(busiest / tokens / depth) * (0.7 + block * up(kb / w)));
-        consider(1.4 + most(passes * megabytes / 6.7, time), {tokens == 16 ? Choice::kStream16 : Choice::kStream64, w, (int)depth});
+        const double passes = most(1.0, r / tokens + (tokens == 16 ? 0.7 : 0.2));
+        const double taken = 32.0 * K * (tokens == 16 ? 1.4 : 2.6 + 1.3 * full) / 35e3 + w / 16.0;
+        const double block = tokens == 16 ? 0.9 : 0.9 + 0.6 * full;
+        const double time = most(up(groups * passes / cus) * taken * (out16 ? 1.0 : 1.25), up(busiest / tokens / depth) * (0.4 + block * up(kb / w)));
+        consider(1.5 + most(passes * megabytes / 6.5, time), {tokens == 16 ? Choice::kStream16 : Choice::kStream64, w, (int)depth});
     }
     auto tiles = [&](int rows, int tokens, double step, double rate, Choice c) {
         const double rounds = up(up(r / tokens) * experts * ((N + rows - 1) / rows) / cus);
@@ -731,9 +748,10 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
     };
     // (the tiles' loads are four and two steps ahead of them)
     const double half = least(r, 128) / 128, full = least(r, 256) / 256;
-    if (kb >= 4) tiles(128, 128, out16 ? 0.8 + 0.2 * half : 1.3, out16 ? 4.8 : 4.1, {Choice::kTiles128, 0, 0});
-    if (kb >= 2) tiles(256, 128, out16 ? 0.8 + 0.58 * half : 1.3 + 0.75 * half, out16 ? 5.6 : 4.0, {Choice::kTiles256x128, 0, 0});
-    if (kb >= 2 && out16) tiles(256, 256, 1.0 + 1.1 * full, 4.9, {Choice::kTiles256, 0, 0});
+    const double wide = r > 32;   // (the second 32 rows of each 64)
+    if (kb >= 4) tiles(128, 128, out16 ? 0.45 + 0.1 * half + 0.2 * wide : 0.75 + 0.1 * half + 0.35 * wide, out16 ? 5.4 : 4.9, {Choice::kTiles128, 0, 0});
+    if (kb >= 2) tiles(256, 128, out16 ? 0.85 + 0.6 * half : 1.4 + 0.6 * half, out16 ? 5.2 : 3.6, {Choice::kTiles256x128, 0, 0});
+    if (kb >= 2 && out16) tiles(256, 256, 1.1 + 0.95 * full, 4.5, {Choice::kTiles256, 0, 0});
     return best;
 }
 
