@@ -330,10 +330,12 @@ int moe_pool_load(const void *store_gate, const void *store_up, const void *stor
  * expert products of their own.  None of the calls below uses the state of a
  * workspace, waits for another workgroup or synchronises: calls on different
  * streams may run at the same time (with a workspace each, where one is
- * taken), and each can be captured into a graph.  T*k <= 2^30; sizes beyond
- * the limits are MOE_ERR_SHAPE.  Pointers to rows are 16-byte aligned, widths
- * multiples of 8 (MOE_ERR_ALIGN).  x_bf16, rows_bf16, out_bf16, w_bf16:
- * elements are bf16 (non-zero) or fp32 (0). */
+ * taken), and each can be captured into a graph.  T*k, rows <= 2^30; sizes
+ * beyond the limits are MOE_ERR_SHAPE.  Pointers to rows are 16-byte aligned,
+ * widths multiples of 8 (MOE_ERR_ALIGN).  Outputs do not overlap inputs.
+ * x_bf16, rows_bf16, out_bf16, w_bf16: elements are bf16 (non-zero) or fp32
+ * (0).  (moe_route_topk takes T*E <= 65536: a longer batch is routed in
+ * pieces, each into its part of topk_idx and topk_w, and sorted as one.) */
 
 /* Assignments sorted by expert (stable).  ids [T,k] int32: experts
  * (topk_idx) or slots (slot_idx); values outside [0,E) are assignments of no
@@ -380,7 +382,8 @@ int moe_unpermute_backward(const void *dout, int dout_bf16, const void *rows, in
  *   scale = m / 448,   q = x * (448 / m) rounded to nearest, ties to even,
  * x = scale * q.  A block with NaN gets the scale NaN, one with an infinity
  * the scale infinity and NaN in the infinity's place.  A row of K values
- * (K % 8 == 0) takes Kp = 128 * ceil(K/128) bytes, zero behind the K-th.
+ * (K % 8 == 0, K <= 2^24) takes Kp = 128 * ceil(K/128) bytes, zero behind
+ * the K-th.
  *
  * Rows: x [M,K] -> q [M,Kp], scale [M,Kp/128], blocks of 128 of a row.
  * n_rows: device pointer to the number of rows that hold something (offsets + E
@@ -404,9 +407,11 @@ int moe_quantize_weights_fp8(const void *w, int w_bf16, int E, int N, int K, voi
  * [0,M]; out [M,N].  Rows of no expert are left as they were.  fp32 results:
  * sums in 32 bits throughout.  bf16 results: the 128 products of a block are
  * added by the 8-bit matrix instruction, which cuts the smaller ones of each
- * eight at 2^-13 of the largest (about 2e-5 of the results' norm).  E <= 1024;
- * E = 1 with offsets {0, M} is the plain product.  The gradient to x is the
- * same call on the quantised gradient and the transposed weights. */
+ * eight at 2^-13 of the largest (about 2e-5 of the results' norm).  E <= 1024,
+ * N <= 2^24, K <= 2^20; E = 1 with offsets {0, M} is the plain product.  The
+ * gradient to x is the same call on the quantised gradient and the transposed
+ * weights.  An element is the same from call to call; between calls of other
+ * sizes the order of its sum may differ. */
 int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const void *w, const float *w_scale,
                            const int32_t *offsets, int M, int N, int K, int E, void *out, int out_bf16, void *stream);
 

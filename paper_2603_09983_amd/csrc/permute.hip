@@ -3,7 +3,8 @@
 //
 // Sort: a counting sort, stable, so that a row's place follows from the routing alone.  Rows of expert e are
 // [offsets[e], offsets[e+1]), inside them the flat assignment ids ascend.  Assignments of no expert (-1) come to no row.
-// Moving and summing rows: bound by memory; every row is read once and written once, 16 bytes a lane.
+// Moving and summing rows: bound by memory; every row is read once and written once, 16 bytes a lane.  (A large copy of this card's
+// memory moves 4.95 TB/s, read and written; the rates below that are higher have reads or writes that outweigh the other.)
 #include "../../include/moe_spac.h"
 #include "rows_device.h"
 
@@ -14,6 +15,8 @@ namespace {
 using namespace rows;
 
 // ---- sort ----
+// Bound by latency: up to 4096 assignments one workgroup and one launch (6 assignments 3.1 us, 4000 on 60 experts 6.0), then a count and
+// a place launch over up to 128 workgroups (98304 on 64 experts 4.8 + 5.9 us; their 1.2 MB are 0.2 us of memory).
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortBlocks = 128;      // most workgroups of the two-launch form
 constexpr int kSortChunk = 1024;      // least assignments of one of its workgroups (98304 on 64 experts: 8.2 us; 2048 8.4, 4096 8.9)
@@ -173,7 +176,8 @@ struct MoveArgs {
     unsigned parts, rcp_parts, items;
 };
 
-// out[pos[t,j]] = x[t]: a wavefront has U words a lane of one token's row and stores them k times.
+// out[pos[t,j]] = x[t]: a wavefront has U words a lane of one token's row and stores them k times.  1000 tokens of 2040 floats to some 2600
+// rows: 7.4 us, 4.0 TB/s; U = 4 as soon as that leaves a wavefront for each SIMD, else 1, so that few tokens spread over more of them.
 template <int U>
 __global__ __launch_bounds__(kRowThreads) void permute_kernel(MoveArgs a)
 {
@@ -206,7 +210,8 @@ struct MoveFp8Args {
     unsigned blocks, rcp_blocks, items;   // blocks of a row; T * blocks
 };
 
-// The same with the row quantised on the way: eight lanes have a block of 128, sixteen values a lane.
+// The same with the row quantised on the way: eight lanes have a block of 128, sixteen values a lane.  A row is read and quantised once and
+// stored k times: 16384 tokens of 2048 bf16 to 98304 rows of 2048 bytes 43.5 us, 6.3 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(kRowThreads) void permute_fp8_kernel(MoveFp8Args a)
 {
@@ -269,7 +274,8 @@ __device__ __forceinline__ void store8(u32x4 *row, int unit, const float *f, int
     }
 }
 
-// out[t] (+)= sum over j of w[t,j] rows[pos[t,j]], in fp32, j ascending: a wavefront has eight columns a lane of one token.
+// out[t] (+)= sum over j of w[t,j] rows[pos[t,j]], in fp32, j ascending: a wavefront has eight columns a lane of one token, so that a
+// result is one lane's sum, in the same order whatever the sizes.  8192 tokens of 2048 from six bf16 rows each, to bf16: 46 us, 5.1 TB/s.
 template <bool IN16, bool OUT16>
 __global__ __launch_bounds__(kRowThreads) void unpermute_kernel(SumArgs a)
 {
@@ -309,7 +315,8 @@ struct BackArgs {
     unsigned A, rcp_k;
 };
 
-// drows[pos[t,j]] = w[t,j] dout[t], dw[t,j] = <dout[t], rows[pos[t,j]]>: a wavefront has one assignment.
+// drows[pos[t,j]] = w[t,j] dout[t], dw[t,j] = <dout[t], rows[pos[t,j]]>: a wavefront has one assignment, so that the scalar product needs
+// no second pass and no atomics; dout comes k times, all but the first from L2.  4096 tokens of 4096 bf16, k = 2: 34 us, 4.9 TB/s.
 template <bool OUT16, bool IN16>
 __global__ __launch_bounds__(kRowThreads) void unpermute_backward_kernel(BackArgs a)
 {
