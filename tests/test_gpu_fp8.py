@@ -282,3 +282,60 @@ def test_gradient_to_the_rows_is_the_transposed_product():
                            for e, (lo, hi) in enumerate(zip(offsets, offsets[1:])))
         slope = (at(1.0) - at(-1.0)) / 2
     assert abs(slope - float((got * step).sum())) <= float((R.matmul_bound(size, x.grad, N, torch.float32) * step.abs()).sum())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("counts,N,K", [([i * i % 41 for i in range(1024)], 264, 512), ([i * i % 41 for i in range(1000)], 264, 256)], ids=["1024x512", "1000x256"])
+def test_tiles_of_as_many_experts_as_there_can_be(counts, N, K, dtype):
+    _check(*_operands(counts, N, K, 15, lead=1, tail=1), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_product_of_rows_behind_4_gib(dtype):
+    """The last rows of 5 GB, results behind 4 GiB; the rows before them are no expert's."""
+    K, M, N = 8192, 600000, 4096
+    a, sa, w, sw, _ = _operands([70], N, K, 16)
+    x, sx = torch.zeros(M, K, dtype=torch.uint8, device="cuda"), torch.zeros(M, K // 128, device="cuda")
+    x[-70:], sx[-70:] = a.view(torch.uint8).cuda(), sa.cuda()
+    out = torch.full((M, N), 77.0, dtype=dtype, device="cuda")
+    offsets = torch.tensor([M - 70, M], dtype=torch.int32)
+    B.moe_grouped_matmul_fp8(x, sx, w.cuda(), sw.cuda(), offsets.cuda(), M, N, K, 1, out, dtype == torch.bfloat16)
+    assert bool((out[:-70] == 77.0).all())
+    want, size = R.matmul(a, sa, w, sw, torch.tensor([0, 70]))
+    assert bool(((out[-70:].cpu().double() - want).abs() <= R.matmul_bound(size, want, K, dtype)).all())
+
+
+@pytest.mark.parametrize("rows", [3, 40, 200, 700])
+def test_product_with_weights_behind_4_gib(rows):
+    """The last of 70 experts of 8192 x 8192, whose weights begin behind 4 GiB."""
+    N = K = 8192
+    E, dtype = 70, torch.bfloat16
+    a, sa, w, sw, _ = _operands([rows], N, K, 17)
+    all_w, all_s = torch.zeros(E, N, K, dtype=torch.uint8, device="cuda"), torch.zeros(E, N // 128, K // 128, device="cuda")
+    all_w[-1], all_s[-1] = w[0].view(torch.uint8).cuda(), sw[0].cuda()
+    offsets = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    offsets[-1] = rows
+    out = torch.full((rows, N), 77.0, dtype=dtype, device="cuda")
+    B.moe_grouped_matmul_fp8(a.cuda(), sa.cuda(), all_w, all_s, offsets, rows, N, K, E, out, True)
+    want, size = R.matmul(a, sa, w, sw, torch.tensor([0, rows]))
+    assert bool(((out.cpu().double() - want).abs() <= R.matmul_bound(size, want, K, dtype)).all())
+
+
+def test_quantisers_behind_4_gib():
+    """The last rows and matrices of tensors of 5 to 10 GB."""
+    M, K = 600000, 8192
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    rows = _values(9, K, 18, torch.bfloat16)
+    x[-9:] = rows.cuda()
+    q, scale = torch.empty(M, K, dtype=torch.uint8, device="cuda"), torch.empty(M, K // 128, device="cuda")
+    B.moe_quantize_fp8(x, True, None, M, K, q, scale)
+    wq, ws = R.blocks(rows)
+    assert torch.equal(q[-9:].cpu(), wq.view(torch.uint8)) and torch.equal(scale[-9:].cpu(), ws) and not q[:-9].any()
+    E = 70
+    w = torch.zeros(E, K, K, dtype=torch.bfloat16, device="cuda")
+    last = torch.randn(K, K, generator=torch.Generator().manual_seed(19)).bfloat16()
+    w[-1] = last.cuda()
+    q, scale = torch.empty(E, K, K, dtype=torch.uint8, device="cuda"), torch.empty(E, K // 128, K // 128, device="cuda")
+    B.moe_quantize_weights_fp8(w, True, E, K, K, q, scale)
+    wq, ws = R.blocks(last, tall=True)
+    assert torch.equal(q[-1].cpu(), wq.contiguous().view(torch.uint8)) and torch.equal(scale[-1].cpu(), ws) and not q[:-1].any()
