@@ -6,6 +6,7 @@
 #include "../../include/moe_spac.h"
 #include "rows_device.h"
 #include <math.h>
+#include <type_traits>
 
 namespace moe {
 
@@ -23,7 +24,7 @@ struct MatmulArgs {
     void *out;                   // [M,N]
     int M, N, K, E;
     int scale_words;             // the rows' scales are whole 16-byte words
-    int by_row;                  // (stream_matmul_kernel) workgroups for each row instead of for each expert
+    int by_row;                  // (stream_matmul_kernel) workgroups for each row instead of for each expert's groups
 };
 
 __device__ __forceinline__ int clamped(int v, int most) { return v < 0 ? 0 : v > most ? most : v; }
@@ -82,12 +83,13 @@ __device__ __forceinline__ f32x4 mfma128(const Operand<true> &a, const Operand<t
 // ---- few rows to an expert: its weights streamed past them ----
 // Bound by the weights' bytes.  A workgroup has 32 weight rows of one expert against its tokens, 16 T at a time; its wavefronts share
 // the columns, block by block (neighbouring wavefronts have neighbouring blocks: together they read consecutive columns), and their
-// sums meet in LDS in a fixed order.  gridDim.z workgroups take an expert's tokens in turn, so that an expert that has many (routing is
-// uneven, and the host does not know how) does not keep everybody waiting.  A wavefront has U blocks in flight: 32 rows x 128 columns of
-// weights, 16 T x 128 of rows (which all workgroups of the expert read: from L2).
-// 27 rows on 18 of 64 experts of 2816 x 2048: 20 us, 5.4 TB/s; 2 rows on 8 of 4096 x 14336: 21.7 us, 5.4 TB/s, launch included.
-template <bool OUT16, int T>
-constexpr int kMostWaves = OUT16 && T == 1 ? 16 : 8;   // (so that what is in flight has the registers)
+// sums meet in LDS in a fixed order.  Each 16 T tokens of an expert have workgroups of their own, so that one that has many (routing is
+// uneven, and the host does not know how) keeps nobody waiting: those of the first 16 T go by the expert, the others are found from all
+// counts.  (All of them found so: 128 rows on 256 experts of 2048 x 1024 46 instead of 34 us.  Workgroups by the mean count, in turn over
+// an expert's rows: 650 skewed rows on 256 experts of 384 x 1088 33 us instead of 12.)  A wavefront has U blocks in flight: 32 rows x 128
+// columns of weights, 16 T x 128 of rows (which all workgroups of the expert read: from L2).
+// 27 rows on 18 of 64 experts of 2816 x 2048: 18 us, 6.0 TB/s; 2 rows on 8 of 4096 x 14336: 20 us, 5.9 TB/s, launch included.
+constexpr int kMostWaves = 8;
 
 // A load instruction takes eight rows' whole 128 columns (16 rows x 64 columns, as the matrix instruction has them, reach 5.8 TB/s, and
 // without the hint that they are read once only, or each line would come twice; eight rows 6.2 TB/s with it): lanes 0 to 7 of sixteen
@@ -104,109 +106,156 @@ __device__ __forceinline__ void exchange(u32x4 *v, bool upper)
     }
 }
 
+// The i-th group of ROWS rows behind the experts' first groups: expert and first row; all wavefronts work out the same.  Sums over the
+// lanes by register rotations.
+struct Group {
+    int e, r0, end;   // e < 0: there are not so many
+};
+template <int ROWS>
+__device__ __forceinline__ Group later_group(const int32_t *offsets, int M, int E, int i)
+{
+    constexpr int n = 4;   // experts of a lane
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int e = 0; e < E; e += n * kWave) {
+        int at[n + 1], up = 0;
+#pragma unroll
+        for (int k = 0; k <= n; ++k) at[k] = clamped(offsets[e + n * lane + k < E ? e + n * lane + k : E], M);
+#pragma unroll
+        for (int k = 0; k < n; ++k) up += at[k] < at[k + 1] ? (at[k + 1] - at[k] - 1) / ROWS : 0;
+        const int mine = up;   // (and up: with those of the lanes before)
+        up += __builtin_amdgcn_update_dpp(0, up, 0x111, 0xf, 0xf, false);   // one to the right in each row of sixteen lanes, two, four, eight
+        up += __builtin_amdgcn_update_dpp(0, up, 0x112, 0xf, 0xf, false);
+        up += __builtin_amdgcn_update_dpp(0, up, 0x114, 0xf, 0xf, false);
+        up += __builtin_amdgcn_update_dpp(0, up, 0x118, 0xf, 0xf, false);
+        up += __builtin_amdgcn_update_dpp(0, up, 0x142, 0xa, 0xf, false);   // a row's last lane to the next row, the second's to the upper half
+        up += __builtin_amdgcn_update_dpp(0, up, 0x143, 0xc, 0xf, false);
+        const unsigned long long behind = __ballot(up > i);
+        if (behind) {
+            const int l = __builtin_ctzll(behind);
+            i -= __builtin_amdgcn_readlane(up - mine, l);
+#pragma unroll
+            for (int k = 0; k < n; ++k) {
+                const int lo = __builtin_amdgcn_readlane(at[k], l), hi = __builtin_amdgcn_readlane(at[k + 1], l);
+                const int groups = lo < hi ? (hi - lo - 1) / ROWS : 0;
+                if (i < groups) return Group{e + n * l + k, lo + (i + 1) * ROWS, hi};
+                i -= groups;
+            }
+        }
+        i -= __builtin_amdgcn_readlane(up, kWave - 1);
+    }
+    return Group{-1, 0, 0};
+}
+
 template <bool OUT16, int T, int U>
-__global__ __launch_bounds__((kMostWaves<OUT16, T>)*kWave) void stream_matmul_kernel(MatmulArgs a)
+__global__ __launch_bounds__(kMostWaves *kWave) void stream_matmul_kernel(MatmulArgs a)
 {
     extern __shared__ __align__(16) uint8_t lds[];
     f32x4 *const part = (f32x4 *)lds;   // [wavefront][2 T][lane]
-    int e = blockIdx.y;
-    const int n0 = blockIdx.x * 32;
-    if (a.by_row) {   // blockIdx.y is a row, and the workgroup of an expert's first row is the expert's
-        __shared__ int found;
-        if (threadIdx.x == 0) found = -1;
-        __syncthreads();
-        for (int i = threadIdx.x; i < a.E; i += blockDim.x)
-            if (clamped(a.offsets[i], a.M) == e && clamped(a.offsets[i + 1], a.M) > e) found = i;
-        __syncthreads();
-        e = __builtin_amdgcn_readfirstlane(found);
-        if (e < 0) return;
-    }
-    const int lo = clamped(a.offsets[e], a.M), hi = clamped(a.offsets[e + 1], a.M);
-    if (lo + (int)blockIdx.z * 16 * T >= hi) return;
     const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock;
+    const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock, n0 = blockIdx.x * 32;
+    const bool upper = col >= 8;
+    Group g = {(int)(blockIdx.z * gridDim.y + blockIdx.y), 0, 0};
+    if (a.by_row) {   // workgroups for the rows, of which those of a group's first row are the group's
+        int *const found = (int *)lds;   // (its place is part's afterwards)
+        const int row = g.e;
+        if (threadIdx.x == 0) *found = -1;
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.E; i += blockDim.x) {
+            const int lo = clamped(a.offsets[i], a.M);
+            if (lo <= row && row < clamped(a.offsets[i + 1], a.M) && (row - lo) % (16 * T) == 0) *found = i;
+        }
+        __syncthreads();
+        g = Group{*found, row, *found < 0 ? 0 : clamped(a.offsets[*found + 1], a.M)};
+        __syncthreads();
+    } else if (g.e >= a.E) {
+        g = later_group<16 * T>(a.offsets, a.M, a.E, g.e - a.E);
+    } else {
+        g.r0 = clamped(a.offsets[g.e], a.M), g.end = clamped(a.offsets[g.e + 1], a.M);
+    }
+    const int e = __builtin_amdgcn_readfirstlane(g.e), r0 = __builtin_amdgcn_readfirstlane(g.r0), hi = __builtin_amdgcn_readfirstlane(g.end);
+    if (e < 0 || r0 >= hi) return;
     const uint8_t *wrow[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
         const int n = n0 + 8 * m + (col & 7) < a.N ? n0 + 8 * m + (col & 7) : a.N - 1;
         wrow[m] = a.w + ((size_t)e * a.N + n) * a.K + grp * 32 + (col >> 3) * 16;
     }
-    const bool upper = col >= 8;
     const float *const sw = a.w_scale + ((size_t)e * ((a.N + kBlock - 1) / kBlock) + n0 / kBlock) * kb;
-    for (int r0 = lo + (int)blockIdx.z * 16 * T; r0 < hi; r0 += (int)gridDim.z * 16 * T) {
-        const uint8_t *xrow[T];
-        const float *sx[T];
+    const uint8_t *xrow[T];
+    const float *sx[T];
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            const int r = r0 + 16 * t + col < hi ? r0 + 16 * t + col : hi - 1;
-            xrow[t] = a.a + (size_t)r * a.K + grp * 32;
-            sx[t] = a.a_scale + (size_t)r * kb;
-        }
-        f32x4 acc[2][T];
+    for (int t = 0; t < T; ++t) {
+        const int r = r0 + 16 * t + col < hi ? r0 + 16 * t + col : hi - 1;
+        xrow[t] = a.a + (size_t)r * a.K + grp * 32;
+        sx[t] = a.a_scale + (size_t)r * kb;
+    }
+    f32x4 acc[2][T];
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int t = 0; t < T; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int b0 = w; b0 < kb; b0 += U * waves) {
-            u32x4 y[U][2][2], x[U][T][2];
-            float s[U][T];
-            const int n = (kb - 1 - b0) / waves + 1;   // blocks of this round that there are
+        for (int t = 0; t < T; ++t) acc[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Blocks b0, b0 + waves, .. (count of them): all their loads are on their way before the first is used.
+    auto blocks = [&](auto count, int b0) {
+        constexpr int n = decltype(count)::value;
+        u32x4 y[n][2][2], x[n][T][2];
+        float sx_of[n][T], sw_of[n];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (u < n) {
-                    const size_t at = (size_t)(b0 + u * waves) * kBlock;
+        for (int u = 0; u < n; ++u) {
+            const size_t at = (size_t)(b0 + u * waves) * kBlock;
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        y[u][m][0] = __builtin_nontemporal_load((const u32x4 *)(wrow[2 * m] + at));
-                        y[u][m][1] = __builtin_nontemporal_load((const u32x4 *)(wrow[2 * m + 1] + at));
-                    }
-#pragma unroll
-                    for (int t = 0; t < T; ++t) {
-                        x[u][t][0] = *(const u32x4 *)(xrow[t] + at);
-                        x[u][t][1] = *(const u32x4 *)(xrow[t] + at + 16);
-                        s[u][t] = sx[t][b0 + u * waves] * sw[b0 + u * waves];
-                    }
-                }
+            for (int m = 0; m < 2; ++m) {
+                y[u][m][0] = __builtin_nontemporal_load((const u32x4 *)(wrow[2 * m] + at));
+                y[u][m][1] = __builtin_nontemporal_load((const u32x4 *)(wrow[2 * m + 1] + at));
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (u < n) {
-                    exchange(y[u][0], upper);
-                    exchange(y[u][1], upper);
-                    const Operand<!OUT16> w0(y[u][0][0], y[u][0][1]), w1(y[u][1][0], y[u][1][1]);
-#pragma unroll
-                    for (int t = 0; t < T; ++t) {
-                        const Operand<!OUT16> xo(x[u][t][0], x[u][t][1]);
-                        const f32x4 p0 = mfma128(w0, xo), p1 = mfma128(w1, xo);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            acc[0][t][i] = __builtin_fmaf(p0[i], s[u][t], acc[0][t][i]);
-                            acc[1][t][i] = __builtin_fmaf(p1[i], s[u][t], acc[1][t][i]);
-                        }
-                    }
-                }
+            for (int t = 0; t < T; ++t) {
+                x[u][t][0] = *(const u32x4 *)(xrow[t] + at);
+                x[u][t][1] = *(const u32x4 *)(xrow[t] + at + 16);
+                sx_of[u][t] = sx[t][b0 + u * waves];
             }
+            sw_of[u] = sw[b0 + u * waves];
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int u = 0; u < n; ++u) {
+            exchange(y[u][0], upper);
+            exchange(y[u][1], upper);
+            const Operand<!OUT16> w0(y[u][0][0], y[u][0][1]), w1(y[u][1][0], y[u][1][1]);
 #pragma unroll
-            for (int t = 0; t < T; ++t) part[(w * 2 * T + 2 * t + m) * kWave + lane] = acc[m][t];
-        __syncthreads();
-        for (int i = w; i < 2 * T; i += waves) {
-            f32x4 sum = part[i * kWave + lane];
-            for (int v = 1; v < waves; ++v) sum += part[(v * 2 * T + i) * kWave + lane];
-            const int r = r0 + 16 * (i >> 1) + col, n = n0 + 16 * (i & 1) + 4 * grp;   // (N is a multiple of 8)
-            if (r < hi && n < a.N) {
-                const size_t at = (size_t)r * a.N + n;
-                if (OUT16) {
-                    const u32x2 v = {pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
-                    *(u32x2 *)((uint16_t *)a.out + at) = v;
-                } else {
-                    *(f32x4 *)((float *)a.out + at) = sum;
+            for (int t = 0; t < T; ++t) {
+                const Operand<!OUT16> xo(x[u][t][0], x[u][t][1]);
+                const f32x4 p0 = mfma128(w0, xo), p1 = mfma128(w1, xo);
+                const float s = sx_of[u][t] * sw_of[u];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    acc[0][t][i] = __builtin_fmaf(p0[i], s, acc[0][t][i]);
+                    acc[1][t][i] = __builtin_fmaf(p1[i], s, acc[1][t][i]);
                 }
             }
         }
-        __syncthreads();
+    };
+    int b0 = w;
+    for (; b0 + (U - 1) * waves < kb; b0 += U * waves) blocks(std::integral_constant<int, U>(), b0);
+    if (U > 1)
+        for (; b0 < kb; b0 += waves) blocks(std::integral_constant<int, 1>(), b0);
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 0; t < T; ++t) part[(w * 2 * T + 2 * t + m) * kWave + lane] = acc[m][t];
+    __syncthreads();
+    for (int i = w; i < 2 * T; i += waves) {
+        f32x4 sum = part[i * kWave + lane];
+        for (int v = 1; v < waves; ++v) sum += part[(v * 2 * T + i) * kWave + lane];
+        const int r = r0 + 16 * (i >> 1) + col, n = n0 + 16 * (i & 1) + 4 * grp;   // (N is a multiple of 8)
+        if (r < hi && n < a.N) {
+            const size_t at = (size_t)r * a.N + n;
+            if (OUT16) {
+                const u32x2 v = {pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+                *(u32x2 *)((uint16_t *)a.out + at) = v;
+            } else {
+                *(f32x4 *)((float *)a.out + at) = sum;
+            }
+        }
     }
 }
 
@@ -215,7 +264,7 @@ __global__ __launch_bounds__((kMostWaves<OUT16, T>)*kWave) void stream_matmul_ke
 // A wavefront has 64 weight rows x 128 (64) tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core) four multiply-adds (16
 // cycles of the vector ALU) bring the block's sum, times its scales, into the tile's.
 //
-// Bound by the matrix cores and by the power that they and the loads draw together.  49152 rows on 64 experts of 2816 x 2048, bf16: 330 us,
+// Bound by the matrix cores and by the power that they and the loads draw together.  49152 rows on 64 experts of 2816 x 2048, bf16: 322 us,
 // 1.7 PFLOP/s; the products and multiply-adds alone, on random values, run at 3.1 (2.1 GHz), with the loads and stores the clock falls
 // to 1.7 GHz, the matrix cores are busy 44 % of the cycles, and one tile in seven has few rows.
 //
@@ -699,23 +748,22 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
 // Which kernel takes a call: the one that should be the fastest by what they measured, from the sizes alone.  us, bf16 results / fp32; r:
 // rows an expert, evenly.  64 experts of 2816 x 2048, then one of them, then 8 of 512 x 7168:
 //            r = 6         12        24        47        94        187       281       768          64        512       12        265
-//      16 rows   62/67     77/83     145/152   254/262   491/507   955/975   1433/-    -            12/13     -         16/15     126/122
-//      64 rows   86/99     91/108    108/123   142/153   277/297   506/539   748/792   -            12/12     -         18/19     76/78
-//      128 x 128 70/72     72/75     74/81     81/92     92/129    144/241   195/327   434/737      13/18     16/26     25/34     40/69
-//      256 x 128 69/74     70/77     74/81     78/89     89/120    142/213   176/278   358/610      16/25     22/37     43/68     57/104
-//      256 x 256 72/-      73/-      76/-      80/-      90/-      114/-     187/-     322/-        20/-      31/-      55/-      84/-
+//      16 rows   63/62     76/79     146/148   241/242   441/447   851/854   1251/-    -            10/11     -         15/16     103/102
+//      64 rows   81/84     90/95     108/109   141/143   276/282   505/511   752/763   -            11/12     -         18/18     80/83
+//      128 x 128 71/73     72/75     74/81     81/93     92/127    144/239   197/330   446/755      13/18     16/26     25/34     40/69
+//      256 x 128 69/75     71/78     73/81     78/89     89/119    141/212   177/279   362/616      16/25     22/37     43/68     57/104
+//      256 x 256 72/-      73/-      76/-      80/-      90/-      117/-     191/-     335/-        20/-      31/-      55/-      84/-
 // (16 and 64 rows: the streaming kernels; the others: tiles of weight rows x rows.  256 x 256 with fp32 results, whose operands are wider
-// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3800 calls of random sizes the choice took 1.035 times
-// the fastest's time, 1.055 where the routing was skewed, which it does not see; without one of the kernels the fastest took 1.006
-// (256 x 256) to 1.04 (16 rows, 128 x 128) times as long as with all.
+// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3000 calls of random sizes the choice took 1.035 times
+// the fastest's time, 1.043 where the routing was skewed, which it does not see; without one of the kernels the fastest took 1.006 (64
+// rows, 256 x 256) to 1.06 (16 rows) times as long as with all.
 //
 // All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernels: what a CU
-// takes in, weights and rows, at 35 B/ns; or the blocks that a wavefront loads one after the other (0.9 us, 1.5 for 64 rows that
-// differ) in each pass over a busy expert's rows.  The tiles: rounds of them over the CUs, each as many steps as there are blocks, a
-// step's time by how many of its rows there are.
+// takes in, weights and rows, at 32 B/ns; or the blocks that a wavefront loads one after the other.  The tiles: rounds of them over the
+// CUs, each as many steps as there are blocks, a step's time by how many of its rows there are.
 struct Choice {
     enum { kStream16, kStream64, kTiles128, kTiles256x128, kTiles256 } kernel;
-    int waves, depth;    // the streaming kernels' wavefronts, and workgroups to an expert's rows
+    int waves;    // of a workgroup of the streaming kernels
 };
 
 Choice choose(int M, int N, int K, int E, bool out16, int cus)
@@ -726,8 +774,6 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
     const double kb = K / kBlock;
     const double experts = E * (1 - exp(-(double)M / E));   // that have rows, where each row is anybody's
     const double r = M / experts, groups = experts * ((N + 31) / 32), megabytes = experts * N * K * 1e-6;
-    // an expert with four times the mean has workgroups for all its rows; one with six times the mean is reckoned with
-    const double busy = least(M, 4 * r), busiest = least(M, 6 * r);
     Choice best = {};
     double least_time = 1e30;
     auto consider = [&](double time, Choice c) {
@@ -737,26 +783,26 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
         }
     };
     for (int tokens = 16; tokens <= 64; tokens *= 4) {
-        int w = 4;   // wavefronts: sixteen to a CU, as far as the columns go round
-        const int w_most = tokens == 64 || !out16 ? 8 : 16;
-        while (w < w_most && groups * w < cus * 16.0 && kb >= 2 * w) w *= 2;
-        const double depth = least(8, up(busy / tokens)), full = least(r, 64) / 64;
-        const double passes = most(1.0, r / tokens + (tokens == 16 ? 0.7 : 0.2));
-        const double taken = 32.0 * K * (tokens == 16 ? 1.4 : 2.6 + 1.3 * full) / 35e3 + w / 16.0;
-        const double block = tokens == 16 ? 0.9 : 0.9 + 0.6 * full;
-        const double time = most(up(groups * passes / cus) * taken * (out16 ? 1.0 : 1.25), up(busiest / tokens / depth) * (0.4 + block * up(kb / w)));
-        consider(1.5 + most(passes * megabytes / 6.5, time), {tokens == 16 ? Choice::kStream16 : Choice::kStream64, w, (int)depth});
+        // Wavefronts: eight where four would have many blocks each or leave CUs without enough of them (1 token on 64 experts of
+        // 2816 x 2048: 4 wavefronts 10.4 us, 8 11.3; 384 tokens 59 and 69; skewed on 128 of 384 x 7936: 48 and 38)
+        const bool eight = tokens == 64 && !out16 ? kb >= 16 && groups <= cus : kb >= 32 || (kb >= 16 && groups <= 2 * cus);
+        const int w = eight ? kMostWaves : kMostWaves / 2;
+        const double full = least(r, 64) / 64;
+        const double passes = most(1.0, r / tokens + (tokens == 16 ? 0.6 : 0.1));
+        const double taken = groups * passes * 32.0 * K * (tokens == 16 ? 1.3 : 3.4 + 1.3 * full) * (out16 ? 1.0 : 1.3) / (32e3 * cus);
+        const double chain = 1 + (tokens == 16 ? 0.6 : 1.1 + 0.5 * full) * up(kb / w);
+        consider(1.5 + most(most(passes * megabytes / 6.0, taken), chain) + 0.25 * chain, {tokens == 16 ? Choice::kStream16 : Choice::kStream64, w});
     }
     auto tiles = [&](int rows, int tokens, double step, double rate, Choice c) {
         const double rounds = up(up(r / tokens) * experts * ((N + rows - 1) / rows) / cus);
-        consider(3.9 + most(megabytes / rate, rounds * kb * step), c);
+        consider(2.9 + most(megabytes / rate, rounds * kb * step), c);
     };
     // (the tiles' loads are four and two steps ahead of them)
     const double half = least(r, 128) / 128, full = least(r, 256) / 256;
     const double wide = r > 32;   // (the second 32 rows of each 64)
-    if (kb >= 4) tiles(128, 128, out16 ? 0.45 + 0.1 * half + 0.2 * wide : 0.75 + 0.1 * half + 0.35 * wide, out16 ? 5.4 : 4.9, {Choice::kTiles128, 0, 0});
-    if (kb >= 2) tiles(256, 128, out16 ? 0.85 + 0.6 * half : 1.4 + 0.6 * half, out16 ? 5.2 : 3.6, {Choice::kTiles256x128, 0, 0});
-    if (kb >= 2 && out16) tiles(256, 256, 1.1 + 0.95 * full, 4.5, {Choice::kTiles256, 0, 0});
+    if (kb >= 4) tiles(128, 128, out16 ? 0.45 + 0.1 * half + 0.22 * wide : 0.65 + 0.1 * half + 0.25 * wide, out16 ? 5.4 : 3.8, {Choice::kTiles128, 0});
+    if (kb >= 2) tiles(256, 128, out16 ? 0.75 + 0.45 * half : 1.1 + 0.45 * half, out16 ? 5.2 : 2.8, {Choice::kTiles256x128, 0});
+    if (kb >= 2 && out16) tiles(256, 256, 1.0 + 0.85 * full, 3.3, {Choice::kTiles256, 0});
     return best;
 }
 
@@ -797,8 +843,9 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
                                   : (out_bf16 ? (const void *)stream_matmul_kernel<true, 4, 1> : (const void *)stream_matmul_kernel<false, 4, 1>);
     // Where most experts have no rows, workgroups for the rows: those of an expert without rows only come and go, but thousands of
     // them take longer than the search of the one for a row does (6 rows on 64 experts of 2816 x 2048: 11.6 against 12.2 us; 54 rows
-    // 21.9 against 20.0).
-    a.by_row = M <= E / 8;
-    return launch_rows(fn, dim3((N + 31) / 32, a.by_row ? M : E, c.depth), c.waves * kWave, &a, (size_t)c.waves * 2 * (tokens / 16) * kWave * 16, stream,
-                       MOE_KERNEL_MATMUL);
+    // 21.9 against 20.0), and where few stay they leave them two to a CU and others empty (2 rows on 8 of 4096 x 14336: 21 against 32).
+    a.by_row = M <= E / 8 || (M < E && (size_t)M * ((N + 31) / 32) <= (size_t)2 * cus);
+    const int groups = a.by_row ? M : E + (M - 1) / tokens;   // (at most)
+    const dim3 grid((N + 31) / 32, groups < 32768 ? groups : 32768, (groups + 32767) / 32768);
+    return launch_rows(fn, grid, c.waves * kWave, &a, (size_t)c.waves * 2 * (tokens / 16) * kWave * 16, stream, MOE_KERNEL_MATMUL);
 }

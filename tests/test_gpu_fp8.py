@@ -192,6 +192,30 @@ def test_product_few_tiles(counts, N, K, dtype):
     _check(*_operands(counts, N, K, 14, lead=2, tail=3), dtype)
 
 
+# few rows and among many experts one or two that have many: their later rows' workgroups are found from the counts
+SKEWED = [([0] * 500 + [90] + [1] * 200 + [70] + [0] * 300, 264, 2048), ([1] * 255 + [40, 33] + [0] * 254 + [17, 100], 72, 384),
+          ([0] * 600 + [49] + [0] * 300 + [33] + [1] * 20 + [0] * 100, 264, 1024), ([0, 0, 49, 0], 40, 512), ([0] * 60 + [64, 16, 17], 136, 4224)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("counts,N,K", SKEWED, ids=[f"{sum(c)}in{len(c)}x{n}x{k}" for c, n, k in SKEWED])
+def test_product_skewed(counts, N, K, dtype):
+    _check(*_operands(counts, N, K, 20, lead=1, tail=2), dtype)
+
+
+def test_product_of_one_block_and_millions_of_rows():
+    M, N, K = 2200000, 8, 128
+    a, sa, w, sw, _ = _operands([5000], N, K, 21)
+    x, sx = a.view(torch.uint8).cuda().repeat(M // 5000, 1), sa.cuda().repeat(M // 5000, 1)
+    out = torch.empty(M, N, device="cuda")
+    offsets = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    B.moe_grouped_matmul_fp8(x, sx, w.cuda(), sw.cuda(), offsets, M, N, K, 1, out, False)
+    got = out.reshape(-1, 5000, N)
+    assert torch.equal(got, got[:1].expand_as(got))
+    want, size = R.matmul(a, sa, w, sw, torch.tensor([0, 5000]))
+    assert bool(((got[0].cpu().double() - want).abs() <= R.matmul_bound(size, want, K, torch.float32)).all())
+
+
 def test_many_rows_rows_of_no_expert_and_nan():
     a, sa, w, sw, offsets = _operands([300, 0, 700], 4104, 512, 13, lead=5, tail=30)
     _check(a, sa, w, sw, offsets, torch.bfloat16)
