@@ -748,21 +748,21 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
 // Which kernel takes a call: the one that should be the fastest by what they measured, from the sizes alone.  us, bf16 results / fp32; r:
 // rows an expert, evenly.  64 experts of 2816 x 2048, then one of them, then 8 of 512 x 7168:
 //            r = 6         12        24        47        94        187       281       768          64        512       12        265
-//      16 rows   63/62     76/79     146/148   241/242   441/447   851/854   1251/-    -            10/11     -         15/16     103/102
-//      64 rows   81/84     90/95     108/109   141/143   276/282   505/511   752/763   -            11/12     -         18/18     80/83
+//      16 rows   60/60     76/77     145/148   239/242   449/446   850/856   1257/1266 -            10/11     -         15/16     104/103
+//      32 rows   65/66     76/78     98/98     188/190   327/329   622/627   915/918   -            8/9       -         15/16     83/83
 //      128 x 128 71/73     72/75     74/81     81/93     92/127    144/239   197/330   446/755      13/18     16/26     25/34     40/69
 //      256 x 128 69/75     71/78     73/81     78/89     89/119    141/212   177/279   362/616      16/25     22/37     43/68     57/104
 //      256 x 256 72/-      73/-      76/-      80/-      90/-      117/-     191/-     335/-        20/-      31/-      55/-      84/-
-// (16 and 64 rows: the streaming kernels; the others: tiles of weight rows x rows.  256 x 256 with fp32 results, whose operands are wider
-// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3000 calls of random sizes the choice took 1.035 times
-// the fastest's time, 1.043 where the routing was skewed, which it does not see; without one of the kernels the fastest took 1.006 (64
-// rows, 256 x 256) to 1.06 (16 rows) times as long as with all.
+// (16 and 32 rows: the streaming kernels; the others: tiles of weight rows x rows.  256 x 256 with fp32 results, whose operands are wider
+// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3000 calls of random sizes the choice took 1.03 to
+// 1.04 times the fastest's time, 1.05 where the routing was skewed, which it does not see; without one of the kernels the fastest took 1.006 (256 x
+// 256) to 1.03 (256 x 128) times as long as with all.
 //
 // All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernels: what a CU
 // takes in, weights and rows, at 32 B/ns; or the blocks that a wavefront loads one after the other.  The tiles: rounds of them over the
 // CUs, each as many steps as there are blocks, a step's time by how many of its rows there are.
 struct Choice {
-    enum { kStream16, kStream64, kTiles128, kTiles256x128, kTiles256 } kernel;
+    enum { kStream16, kStream32, kTiles128, kTiles256x128, kTiles256 } kernel;
     int waves;    // of a workgroup of the streaming kernels
 };
 
@@ -782,27 +782,26 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
             best = c;
         }
     };
-    for (int tokens = 16; tokens <= 64; tokens *= 4) {
-        // Wavefronts: eight where four would have many blocks each or leave CUs without enough of them (1 token on 64 experts of
-        // 2816 x 2048: 4 wavefronts 10.4 us, 8 11.3; 384 tokens 59 and 69; skewed on 128 of 384 x 7936: 48 and 38)
-        const bool eight = tokens == 64 && !out16 ? kb >= 16 && groups <= cus : kb >= 32 || (kb >= 16 && groups <= 2 * cus);
-        const int w = eight ? kMostWaves : kMostWaves / 2;
-        const double full = least(r, 64) / 64;
+    for (int tokens = 16; tokens <= 32; tokens *= 2) {
+        // Wavefronts: eight where four would have many blocks each or leave CUs without enough of them (384 rows on 64 experts of
+        // 2816 x 2048: 4 wavefronts 59 us, 8 69; 4 rows on one of 8192 x 4096: 10.7 and 9.2; 308 skewed on 128 of 384 x 7936: 48 and 38)
+        const int w = kb >= 32 || (kb >= 16 && groups <= 2 * cus) ? kMostWaves : kMostWaves / 2;
+        const double full = least(r, 32) / 32;
         const double passes = most(1.0, r / tokens + (tokens == 16 ? 0.6 : 0.1));
-        const double taken = groups * passes * 32.0 * K * (tokens == 16 ? 1.3 : 3.4 + 1.3 * full) * (out16 ? 1.0 : 1.3) / (32e3 * cus);
-        const double chain = 1 + (tokens == 16 ? 0.6 : 1.1 + 0.5 * full) * up(kb / w);
-        consider(1.5 + most(most(passes * megabytes / 6.0, taken), chain) + 0.25 * chain, {tokens == 16 ? Choice::kStream16 : Choice::kStream64, w});
+        const double taken = groups * passes * 32.0 * K * (tokens == 16 ? 1.35 : 2.0 + 0.6 * full) * (out16 ? 1.0 : 1.2) / (32e3 * cus);
+        const double chain = 0.8 + (tokens == 16 ? 0.6 : 0.8 + 0.3 * full) * up(kb / w);
+        consider(1.5 + most(most(passes * megabytes / 6.0, taken), chain) + 0.25 * chain, {tokens == 16 ? Choice::kStream16 : Choice::kStream32, w});
     }
     auto tiles = [&](int rows, int tokens, double step, double rate, Choice c) {
         const double rounds = up(up(r / tokens) * experts * ((N + rows - 1) / rows) / cus);
-        consider(2.9 + most(megabytes / rate, rounds * kb * step), c);
+        consider(2.5 + most(megabytes / rate, rounds * kb * step), c);
     };
     // (the tiles' loads are four and two steps ahead of them)
     const double half = least(r, 128) / 128, full = least(r, 256) / 256;
     const double wide = r > 32;   // (the second 32 rows of each 64)
-    if (kb >= 4) tiles(128, 128, out16 ? 0.45 + 0.1 * half + 0.22 * wide : 0.65 + 0.1 * half + 0.25 * wide, out16 ? 5.4 : 3.8, {Choice::kTiles128, 0});
-    if (kb >= 2) tiles(256, 128, out16 ? 0.75 + 0.45 * half : 1.1 + 0.45 * half, out16 ? 5.2 : 2.8, {Choice::kTiles256x128, 0});
-    if (kb >= 2 && out16) tiles(256, 256, 1.0 + 0.85 * full, 3.3, {Choice::kTiles256, 0});
+    if (kb >= 4) tiles(128, 128, out16 ? 0.43 + 0.14 * half + 0.27 * wide : 0.48 + 0.1 * half + 0.25 * wide, out16 ? 5.4 : 3.4, {Choice::kTiles128, 0});
+    if (kb >= 2) tiles(256, 128, out16 ? 0.8 + 0.39 * half : 1.1 + 0.37 * half, out16 ? 5.3 : 3.5, {Choice::kTiles256x128, 0});
+    if (kb >= 2 && out16) tiles(256, 256, 1.1 + 0.84 * full, 3.5, {Choice::kTiles256, 0});
     return best;
 }
 
@@ -838,9 +837,9 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
         return tiles((const void *)tile_matmul_kernel<true, 8>, 256, 256, TileSize<8>::kLds);
     default: break;
     }
-    const int tokens = c.kernel == Choice::kStream16 ? 16 : 64;
+    const int tokens = c.kernel == Choice::kStream16 ? 16 : 32;
     const void *fn = tokens == 16 ? (out_bf16 ? (const void *)stream_matmul_kernel<true, 1, 2> : (const void *)stream_matmul_kernel<false, 1, 2>)
-                                  : (out_bf16 ? (const void *)stream_matmul_kernel<true, 4, 1> : (const void *)stream_matmul_kernel<false, 4, 1>);
+                                  : (out_bf16 ? (const void *)stream_matmul_kernel<true, 2, 1> : (const void *)stream_matmul_kernel<false, 2, 1>);
     // Where most experts have no rows, workgroups for the rows: those of an expert without rows only come and go, but thousands of
     // them take longer than the search of the one for a row does (6 rows on 64 experts of 2816 x 2048: 11.6 against 12.2 us; 54 rows
     // 21.9 against 20.0), and where few stay they leave them two to a CU and others empty (2 rows on 8 of 4096 x 14336: 21 against 32).
