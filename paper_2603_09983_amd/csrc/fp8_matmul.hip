@@ -81,13 +81,15 @@ __device__ __forceinline__ f32x4 mfma128(const Operand<true> &a, const Operand<t
 }
 
 // ---- few rows to an expert: its weights streamed past them ----
-// Bound by the weights' bytes.  A workgroup has 32 weight rows of one expert against its tokens, 16 T at a time; its wavefronts share
-// the columns, block by block (neighbouring wavefronts have neighbouring blocks: together they read consecutive columns), and their
-// sums meet in LDS in a fixed order.  Each 16 T tokens of an expert have workgroups of their own, so that one that has many (routing is
-// uneven, and the host does not know how) keeps nobody waiting: those of the first 16 T go by the expert, the others are found from all
-// counts.  (All of them found so: 128 rows on 256 experts of 2048 x 1024 46 instead of 34 us.  Workgroups by the mean count, in turn over
-// an expert's rows: 650 skewed rows on 256 experts of 384 x 1088 33 us instead of 12.)  A wavefront has U blocks in flight: 32 rows x 128
-// columns of weights, 16 T x 128 of rows (which all workgroups of the expert read: from L2).
+// Bound by the weights' bytes.  A workgroup has 32 weight rows of one expert against up to 32 of its rows; its wavefronts share the
+// columns, block by block (neighbouring wavefronts have neighbouring blocks: together they read consecutive columns), and their sums
+// meet in LDS in a fixed order.  Up to 16 rows take one product for each 16 weight rows and two blocks in flight, more of them two and
+// one (rows come from L2, where all workgroups of the expert read them, but through the same load unit: 24 rows on each of 64 experts of
+// 2816 x 2048 in one pass 96 us, in two 145; 6 rows 58, as if there were 32 65).
+// Each 32 rows of an expert have workgroups of their own, so that one that has many (routing is uneven, and the host does not know how)
+// keeps nobody waiting: those of the first 32 go by the expert, the others are found from all counts.  (All of them found so: 128 rows
+// on 256 experts of 2048 x 1024 46 instead of 34 us.  Workgroups by the mean count, in turn over an expert's rows: 650 skewed rows on
+// 256 experts of 384 x 1088 33 instead of 13 us.)
 // 27 rows on 18 of 64 experts of 2816 x 2048: 18 us, 6.0 TB/s; 2 rows on 8 of 4096 x 14336: 20 us, 5.9 TB/s, launch included.
 constexpr int kMostWaves = 8;
 
@@ -146,34 +148,13 @@ __device__ __forceinline__ Group later_group(const int32_t *offsets, int M, int 
     return Group{-1, 0, 0};
 }
 
+// Up to 16 T rows from r0 on (below `end`) of expert e, U blocks in flight.
 template <bool OUT16, int T, int U>
-__global__ __launch_bounds__(kMostWaves *kWave) void stream_matmul_kernel(MatmulArgs a)
+__device__ __forceinline__ void stream_rows(const MatmulArgs &a, f32x4 *part, int e, int r0, int hi)   // part: [wavefront][2 T][lane]
 {
-    extern __shared__ __align__(16) uint8_t lds[];
-    f32x4 *const part = (f32x4 *)lds;   // [wavefront][2 T][lane]
     const int lane = threadIdx.x & (kWave - 1), w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock, n0 = blockIdx.x * 32;
     const bool upper = col >= 8;
-    Group g = {(int)(blockIdx.z * gridDim.y + blockIdx.y), 0, 0};
-    if (a.by_row) {   // workgroups for the rows, of which those of a group's first row are the group's
-        int *const found = (int *)lds;   // (its place is part's afterwards)
-        const int row = g.e;
-        if (threadIdx.x == 0) *found = -1;
-        __syncthreads();
-        for (int i = threadIdx.x; i < a.E; i += blockDim.x) {
-            const int lo = clamped(a.offsets[i], a.M);
-            if (lo <= row && row < clamped(a.offsets[i + 1], a.M) && (row - lo) % (16 * T) == 0) *found = i;
-        }
-        __syncthreads();
-        g = Group{*found, row, *found < 0 ? 0 : clamped(a.offsets[*found + 1], a.M)};
-        __syncthreads();
-    } else if (g.e >= a.E) {
-        g = later_group<16 * T>(a.offsets, a.M, a.E, g.e - a.E);
-    } else {
-        g.r0 = clamped(a.offsets[g.e], a.M), g.end = clamped(a.offsets[g.e + 1], a.M);
-    }
-    const int e = __builtin_amdgcn_readfirstlane(g.e), r0 = __builtin_amdgcn_readfirstlane(g.r0), hi = __builtin_amdgcn_readfirstlane(g.end);
-    if (e < 0 || r0 >= hi) return;
     const uint8_t *wrow[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -257,6 +238,36 @@ __global__ __launch_bounds__(kMostWaves *kWave) void stream_matmul_kernel(Matmul
             }
         }
     }
+}
+
+constexpr int kGroup = 32;   // rows
+
+template <bool OUT16>
+__global__ __launch_bounds__(kMostWaves *kWave) void stream_matmul_kernel(MatmulArgs a)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    Group g = {(int)(blockIdx.z * gridDim.y + blockIdx.y), 0, 0};
+    if (a.by_row) {   // workgroups for the rows, of which those of a group's first row are the group's
+        int *const found = (int *)lds;   // (its place is part's afterwards)
+        const int row = g.e;
+        if (threadIdx.x == 0) *found = -1;
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.E; i += blockDim.x) {
+            const int lo = clamped(a.offsets[i], a.M);
+            if (lo <= row && row < clamped(a.offsets[i + 1], a.M) && (row - lo) % (kGroup) == 0) *found = i;
+        }
+        __syncthreads();
+        g = Group{*found, row, *found < 0 ? 0 : clamped(a.offsets[*found + 1], a.M)};
+        __syncthreads();
+    } else if (g.e >= a.E) {
+        g = later_group<kGroup>(a.offsets, a.M, a.E, g.e - a.E);
+    } else {
+        g.r0 = clamped(a.offsets[g.e], a.M), g.end = clamped(a.offsets[g.e + 1], a.M);
+    }
+    const int e = __builtin_amdgcn_readfirstlane(g.e), r0 = __builtin_amdgcn_readfirstlane(g.r0), hi = __builtin_amdgcn_readfirstlane(g.end);
+    if (e < 0 || r0 >= hi) return;
+    if (hi - r0 > 16) stream_rows<OUT16, 2, 1>(a, (f32x4 *)lds, e, r0, hi);
+    else stream_rows<OUT16, 1, 2>(a, (f32x4 *)lds, e, r0, hi);
 }
 
 // ---- many rows to an expert: tiles of 256 weight rows x 256 tokens (or 128) through LDS ----
@@ -748,22 +759,20 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
 // Which kernel takes a call: the one that should be the fastest by what they measured, from the sizes alone.  us, bf16 results / fp32; r:
 // rows an expert, evenly.  64 experts of 2816 x 2048, then one of them, then 8 of 512 x 7168:
 //            r = 6         12        24        47        94        187       281       768          64        512       12        265
-//      16 rows   60/60     76/77     145/148   239/242   449/446   850/856   1257/1266 -            10/11     -         15/16     104/103
-//      32 rows   65/66     76/78     98/98     188/190   327/329   622/627   915/918   -            8/9       -         15/16     83/83
+//      streaming 60/60     72/73     97/97     184/187   329/329   617/622   903/922   -            8/9       -         15/15     83/83
 //      128 x 128 71/73     72/75     74/81     81/93     92/127    144/239   197/330   446/755      13/18     16/26     25/34     40/69
 //      256 x 128 69/75     71/78     73/81     78/89     89/119    141/212   177/279   362/616      16/25     22/37     43/68     57/104
 //      256 x 256 72/-      73/-      76/-      80/-      90/-      117/-     191/-     335/-        20/-      31/-      55/-      84/-
-// (16 and 32 rows: the streaming kernels; the others: tiles of weight rows x rows.  256 x 256 with fp32 results, whose operands are wider
-// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3000 calls of random sizes the choice took 1.03 to
-// 1.04 times the fastest's time, 1.05 where the routing was skewed, which it does not see; without one of the kernels the fastest took 1.006 (256 x
-// 256) to 1.03 (256 x 128) times as long as with all.
+// (The others than streaming: tiles of weight rows x rows.  256 x 256 with fp32 results, whose operands are wider
+// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3000 calls of random sizes the choice took 1.025
+// times the fastest's time; without one of the kernels the fastest took 1.005 (256 x 256) to 1.14 (streaming) times as long as with all.
 //
-// All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernels: what a CU
+// All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernel: what a CU
 // takes in, weights and rows, at 32 B/ns; or the blocks that a wavefront loads one after the other.  The tiles: rounds of them over the
 // CUs, each as many steps as there are blocks, a step's time by how many of its rows there are.
 struct Choice {
-    enum { kStream16, kStream32, kTiles128, kTiles256x128, kTiles256 } kernel;
-    int waves;    // of a workgroup of the streaming kernels
+    enum { kStream, kTiles128, kTiles256x128, kTiles256 } kernel;
+    int waves;    // of a workgroup of the streaming kernel
 };
 
 Choice choose(int M, int N, int K, int E, bool out16, int cus)
@@ -782,26 +791,24 @@ Choice choose(int M, int N, int K, int E, bool out16, int cus)
             best = c;
         }
     };
-    for (int tokens = 16; tokens <= 32; tokens *= 2) {
-        // Wavefronts: eight where four would have many blocks each or leave CUs without enough of them (384 rows on 64 experts of
-        // 2816 x 2048: 4 wavefronts 59 us, 8 69; 4 rows on one of 8192 x 4096: 10.7 and 9.2; 308 skewed on 128 of 384 x 7936: 48 and 38)
-        const int w = kb >= 32 || (kb >= 16 && groups <= 2 * cus) ? kMostWaves : kMostWaves / 2;
-        const double full = least(r, 32) / 32;
-        const double passes = most(1.0, r / tokens + (tokens == 16 ? 0.6 : 0.1));
-        const double taken = groups * passes * 32.0 * K * (tokens == 16 ? 1.35 : 2.0 + 0.6 * full) * (out16 ? 1.0 : 1.2) / (32e3 * cus);
-        const double chain = 0.8 + (tokens == 16 ? 0.6 : 0.8 + 0.3 * full) * up(kb / w);
-        consider(1.5 + most(most(passes * megabytes / 6.0, taken), chain) + 0.25 * chain, {tokens == 16 ? Choice::kStream16 : Choice::kStream32, w});
-    }
+    // Wavefronts: eight where four would have many blocks each or leave CUs without enough of them (384 rows on 64 experts of
+    // 2816 x 2048: 4 wavefronts 59 us, 8 69; 4 rows on one of 8192 x 4096: 10.7 and 9.2; 308 skewed on 128 of 384 x 7936: 48 and 38)
+    const int w = kb >= 32 || (kb >= 16 && groups <= 2 * cus) ? kMostWaves : kMostWaves / 2;
+    const double more = r <= 8 ? 0 : r >= 24 ? 1 : (r - 8) / 16;   // of the groups of rows, those of more than sixteen
+    const double passes = most(1.0, r / kGroup + 0.2);
+    const double taken = groups * passes * 32.0 * K * (1.38 + 1.9 * more) / (32e3 * cus);
+    const double chain = 0.75 + (0.6 + 0.25 * more) * up(kb / w);
+    consider(1.6 + most(most(passes * megabytes / 6.0, taken), chain) + 0.28 * chain, {Choice::kStream, w});
     auto tiles = [&](int rows, int tokens, double step, double rate, Choice c) {
         const double rounds = up(up(r / tokens) * experts * ((N + rows - 1) / rows) / cus);
-        consider(2.5 + most(megabytes / rate, rounds * kb * step), c);
+        consider(2.3 + most(megabytes / rate, rounds * kb * step), c);
     };
     // (the tiles' loads are four and two steps ahead of them)
     const double half = least(r, 128) / 128, full = least(r, 256) / 256;
     const double wide = r > 32;   // (the second 32 rows of each 64)
-    if (kb >= 4) tiles(128, 128, out16 ? 0.43 + 0.14 * half + 0.27 * wide : 0.48 + 0.1 * half + 0.25 * wide, out16 ? 5.4 : 3.4, {Choice::kTiles128, 0});
-    if (kb >= 2) tiles(256, 128, out16 ? 0.8 + 0.39 * half : 1.1 + 0.37 * half, out16 ? 5.3 : 3.5, {Choice::kTiles256x128, 0});
-    if (kb >= 2 && out16) tiles(256, 256, 1.1 + 0.84 * full, 3.5, {Choice::kTiles256, 0});
+    if (kb >= 4) tiles(128, 128, out16 ? 0.42 + 0.17 * half + 0.25 * wide : 0.68 + 0.11 * half + 0.33 * wide, out16 ? 5.2 : 4.1, {Choice::kTiles128, 0});
+    if (kb >= 2) tiles(256, 128, out16 ? 0.7 + 0.4 * half : 1.3 + 0.28 * half, out16 ? 5.2 : 3.7, {Choice::kTiles256x128, 0});
+    if (kb >= 2 && out16) tiles(256, 256, 1.0 + 0.8 * full, 3.8, {Choice::kTiles256, 0});
     return best;
 }
 
@@ -837,14 +844,12 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
         return tiles((const void *)tile_matmul_kernel<true, 8>, 256, 256, TileSize<8>::kLds);
     default: break;
     }
-    const int tokens = c.kernel == Choice::kStream16 ? 16 : 32;
-    const void *fn = tokens == 16 ? (out_bf16 ? (const void *)stream_matmul_kernel<true, 1, 2> : (const void *)stream_matmul_kernel<false, 1, 2>)
-                                  : (out_bf16 ? (const void *)stream_matmul_kernel<true, 2, 1> : (const void *)stream_matmul_kernel<false, 2, 1>);
     // Where most experts have no rows, workgroups for the rows: those of an expert without rows only come and go, but thousands of
     // them take longer than the search of the one for a row does (6 rows on 64 experts of 2816 x 2048: 11.6 against 12.2 us; 54 rows
     // 21.9 against 20.0), and where few stay they leave them two to a CU and others empty (2 rows on 8 of 4096 x 14336: 21 against 32).
     a.by_row = M <= E / 8 || (M < E && (size_t)M * ((N + 31) / 32) <= (size_t)2 * cus);
-    const int groups = a.by_row ? M : E + (M - 1) / tokens;   // (at most)
+    const int groups = a.by_row ? M : E + (M - 1) / kGroup;   // (at most)
     const dim3 grid((N + 31) / 32, groups < 32768 ? groups : 32768, (groups + 32767) / 32768);
-    return launch_rows(fn, grid, c.waves * kWave, &a, (size_t)c.waves * 2 * (tokens / 16) * kWave * 16, stream, MOE_KERNEL_MATMUL);
+    return launch_rows(out_bf16 ? (const void *)stream_matmul_kernel<true> : (const void *)stream_matmul_kernel<false>, grid, c.waves * kWave, &a,
+                       (size_t)c.waves * 2 * (kGroup / 16) * kWave * 16, stream, MOE_KERNEL_MATMUL);
 }
