@@ -15,13 +15,14 @@ namespace {
 using namespace rows;
 
 // ---- sort ----
-// Bound by latency: up to 4096 assignments one workgroup and one launch (6 assignments 3.1 us, 4000 on 60 experts 6.0), then a count and
-// a place launch over up to 128 workgroups (98304 on 64 experts 4.8 + 5.9 us; their 1.2 MB are 0.2 us of memory).
+// Bound by latency.  Up to 16384 assignments one launch, back to back 3.4 us for 6 assignments, 4.3 for 4000 on 60 experts (one workgroup
+// for them all: 5.6), 5.9 for 16320 on 64 (a count and a place launch: 6.9; 24576: 7.0 either way).  Then the two launches, over up to 128
+// workgroups: 8.3 us for 98304 on 64, whose 1.2 MB are 0.2 us of memory.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr int kSortBlocks = 128;      // most workgroups of the two-launch form
+constexpr int kSortBlocks = 128;      // most workgroups
 constexpr int kSortChunk = 1024;      // least assignments of one of its workgroups (98304 on 64 experts: 8.2 us; 2048 8.4, 4096 8.9)
 constexpr int kAhead = 4;             // loads in flight
-constexpr int kSortOne = 4096;        // up to so many assignments: one workgroup, one launch
+constexpr int kSortOne = 16384;       // up to so many assignments: one launch
 
 struct SortArgs {
     const int32_t *ids;
@@ -54,13 +55,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(SortArgs a)
 // Places of a workgroup's chunk.  A wavefront has a consecutive part of the chunk: the parts' counts, added up over the parts
 // before and the chunks before, say where its first assignment of each expert goes; inside sixty-four assignments the lanes
 // with the same expert find one another by a ballot for each bit of its number.
-// ONE: the only workgroup, which counts for itself.
+// ONE: the only launch, whose workgroups (1024 assignments each) count the whole batch for themselves, each assignment once: into the
+// parts, or as one of the chunks before or behind.
 template <bool ONE>
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
 {
     extern __shared__ int32_t lds[];
     int32_t *part = lds;                            // [kSortWaves][E]: count, then next place
-    int32_t *all = lds + kSortWaves * a.E;          // [E] assignments of the expert in the whole batch
+    int32_t *all = lds + kSortWaves * a.E;          // [E] assignments of the expert in the whole batch (ONE: in the chunks behind)
     int32_t *before = all + a.E;                    // [E] ... in the chunks before
     int32_t *wave_sum = before + a.E;               // [kSortWaves]
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
@@ -69,13 +71,26 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
     const int begin = blockIdx.x * a.chunk, end = begin + a.chunk < a.A ? begin + a.chunk : a.A;
     const int per_wave = a.chunk / kSortWaves;      // (a multiple of 64)
     const int first = begin + w * per_wave, last = first + per_wave < end ? first + per_wave : end;
-    for (int i = first; i < last; i += kAhead * kWave) {
-        int e[kAhead];
+    if (ONE) {   // (a chunk is an assignment a thread)
+        for (int c = 0; c < a.blocks; c += kAhead) {
+            int e[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) e[u] = expert_of(a, i + u * kWave + lane, last);
+            for (int u = 0; u < kAhead; ++u) e[u] = expert_of(a, (c + u) * kSortThreads + tid, a.A);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (e[u] >= 0) atomicAdd(&part[w * a.E + e[u]], 1);
+            for (int u = 0; u < kAhead; ++u) {
+                int32_t *const counts = c + u == (int)blockIdx.x ? part + w * a.E : c + u < (int)blockIdx.x ? before : all;
+                if (e[u] >= 0) atomicAdd(&counts[e[u]], 1);
+            }
+        }
+    } else {
+        for (int i = first; i < last; i += kAhead * kWave) {
+            int e[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) e[u] = expert_of(a, i + u * kWave + lane, last);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (e[u] >= 0) atomicAdd(&part[w * a.E + e[u]], 1);
+        }
     }
     if (!ONE) {
         // the counts of all chunks: a wavefront has every sixteenth row of the table
@@ -100,10 +115,11 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
     // E <= 1024 = threads: thread e has expert e
     int mine = 0;
     if (tid < a.E) {
-        if (ONE)
+        mine = all[tid];
+        if (ONE) {
+            mine += before[tid];
             for (int v = 0; v < kSortWaves; ++v) mine += part[v * a.E + tid];
-        else
-            mine = all[tid];
+        }
     }
     int up = mine;                                  // inclusive sum over the wavefront's lanes
     for (int d = 1; d < kWave; d <<= 1) {
@@ -118,7 +134,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
     for (int v = 0; v < kSortWaves; ++v) valid += wave_sum[v];
     if (tid < a.E) {
         if (blockIdx.x == 0) a.offsets[tid] = at;
-        int next = at + (ONE ? 0 : before[tid]);
+        int next = at + before[tid];
         for (int v = 0; v < kSortWaves; ++v) {
             const int n = part[v * a.E + tid];
             part[v * a.E + tid] = next;
@@ -159,7 +175,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(SortArgs a)
 
 int sort_blocks(int A)
 {
-    if (A <= kSortOne) return 1;
     const int n = (A + kSortChunk - 1) / kSortChunk;
     return n < kSortBlocks ? n : kSortBlocks;
 }
@@ -378,7 +393,7 @@ extern "C" int moe_sort_workspace_bytes(int T, int k, int E, size_t *bytes_out)
 {
     if (!bytes_out) return MOE_ERR_NULL;
     if (T < 1 || k < 1 || E < 1 || E > kMaxC || (size_t)T * k > (size_t)1 << 30) return MOE_ERR_SHAPE;
-    *bytes_out = align256((size_t)sort_blocks(T * k) * E * 4);
+    *bytes_out = align256((size_t)(T * k <= kSortOne ? 1 : sort_blocks(T * k)) * E * 4);
     return MOE_OK;
 }
 
@@ -398,8 +413,8 @@ extern "C" int moe_sort_assignments(const int32_t *ids, int T, int k, int E, int
     const int chunk = ((A + blocks - 1) / blocks + step - 1) / step * step;
     SortArgs a = {ids, A, E, bits, chunk, blocks, offsets, order, pos, (int32_t *)workspace};
     const size_t lds = ((size_t)(kSortWaves + 2) * E + kSortWaves) * 4;
-    const void *place = blocks == 1 ? (const void *)sort_place_kernel<true> : (const void *)sort_place_kernel<false>;
-    if (blocks > 1) {
+    const void *place = A <= kSortOne ? (const void *)sort_place_kernel<true> : (const void *)sort_place_kernel<false>;
+    if (A > kSortOne) {
         rc = launch_rows((const void *)sort_count_kernel, blocks, kSortThreads, &a, (size_t)E * 4, stream, MOE_KERNEL_SORT);
         if (rc) return rc;
     }
