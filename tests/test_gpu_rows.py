@@ -32,6 +32,12 @@ def test_sort(T, k, E, kind):
         assert torch.equal(g.cpu(), want), name
 
 
+@pytest.mark.parametrize("T,k,E,kind", [(T, k, E, kind) for T, k, E in ((16384, 1, 64), (16385, 1, 64), (2730, 6, 1000), (2731, 6, 9), (1023, 2, 1024))
+                                        for kind in ("uniform", "misses", "wild")])
+def test_sort_around_the_ends_of_one_launch(T, k, E, kind):
+    test_sort(T, k, E, kind)
+
+
 def _pos(T, k, extra, seed, misses=True):
     """Distinct rows of T*k + extra at random for the assignments, a few of them outside (negative, beyond the end)."""
     g = torch.Generator().manual_seed(seed)
