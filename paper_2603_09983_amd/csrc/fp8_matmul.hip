@@ -148,7 +148,7 @@ __device__ __forceinline__ Group later_group(const int32_t *offsets, int M, int 
     return Group{-1, 0, 0};
 }
 
-// Up to 16 T rows from r0 on (below `end`) of expert e, U blocks in flight.
+// Up to 16 T rows of expert e, from r0 on and below hi, U blocks in flight.
 template <bool OUT16, int T, int U>
 __device__ __forceinline__ void stream_rows(const MatmulArgs &a, f32x4 *part, int e, int r0, int hi)   // part: [wavefront][2 T][lane]
 {
@@ -240,7 +240,7 @@ __device__ __forceinline__ void stream_rows(const MatmulArgs &a, f32x4 *part, in
     }
 }
 
-constexpr int kGroup = 32;   // rows
+constexpr int kGroup = 32;   // rows of a workgroup
 
 template <bool OUT16>
 __global__ __launch_bounds__(kMostWaves *kWave) void stream_matmul_kernel(MatmulArgs a)
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(kMostWaves *kWave) void stream_matmul_kernel(Matmul
         __syncthreads();
         for (int i = threadIdx.x; i < a.E; i += blockDim.x) {
             const int lo = clamped(a.offsets[i], a.M);
-            if (lo <= row && row < clamped(a.offsets[i + 1], a.M) && (row - lo) % (kGroup) == 0) *found = i;
+            if (lo <= row && row < clamped(a.offsets[i + 1], a.M) && (row - lo) % kGroup == 0) *found = i;
         }
         __syncthreads();
         g = Group{*found, row, *found < 0 ? 0 : clamped(a.offsets[*found + 1], a.M)};
