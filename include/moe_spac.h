@@ -404,14 +404,19 @@ int moe_quantize_weights_fp8(const void *w, int w_bf16, int E, int N, int K, voi
  * for offsets[e] <= r < offsets[e+1], summed in fp32.  x [M,K], w [E,N,K]
  * e4m3 with K a multiple of 128 (the padded width), N a multiple of 8 (else
  * MOE_ERR_ALIGN); offsets [E+1] int32, not descending, values clamped to
- * [0,M]; out [M,N].  Rows of no expert are left as they were.  fp32 results:
- * sums in 32 bits throughout.  bf16 results: the 128 products of a block are
- * added by the 8-bit matrix instruction, which cuts the smaller ones of each
- * eight at 2^-13 of the largest (about 2e-5 of the results' norm).  E <= 1024,
+ * [0,M]; out [M,N].  Rows of no expert are left as they were.  out_bf16: 0
+ * (fp32 results) or non-zero (bf16); sums are kept in 32 bits either way, but
+ * for MOE_BF16_SHORT_SUMS: bf16 results for which calls of many rows may add
+ * the 128 products of a block by the 8-bit matrix instruction, up to twice as
+ * fast.  It cuts the smaller products of each eight consecutive columns at
+ * 2^-13 of the largest: off by 2e-5 of the results' norm on normally
+ * distributed values, and by 7 * 2^-13 of the sum of the products' magnitudes
+ * at most, which is not small beside a sum that cancels.  E <= 1024,
  * N <= 2^24, K <= 2^20; E = 1 with offsets {0, M} is the plain product.  The
  * gradient to x is the same call on the quantised gradient and the transposed
  * weights.  An element is the same from call to call; between calls of other
  * sizes the order of its sum may differ. */
+enum { MOE_BF16_SHORT_SUMS = 2 };   /* a value of out_bf16 */
 int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const void *w, const float *w_scale,
                            const int32_t *offsets, int M, int N, int K, int E, void *out, int out_bf16, void *stream);
 

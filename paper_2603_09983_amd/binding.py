@@ -79,6 +79,7 @@ _lib.moe_quantize_fp8.argtypes = [_vp, _i, _vp, _i, _i] + [_vp] * 3
 _lib.moe_swiglu_fp8.argtypes = [_vp, _i, _vp, _i, _i] + [_vp] * 3
 _lib.moe_quantize_weights_fp8.argtypes = [_vp] + [_i] * 4 + [_vp] * 3
 _lib.moe_grouped_matmul_fp8.argtypes = [_vp] * 5 + [_i] * 4 + [_vp, _i, _vp]
+BF16_SHORT_SUMS = 2   # a value of moe_grouped_matmul_fp8's out_bf16
 ROWS_EXPORTS = ("moe_sort_workspace_bytes", "moe_sort_assignments", "moe_permute", "moe_permute_fp8", "moe_unpermute",
                 "moe_unpermute_backward", "moe_quantize_fp8", "moe_swiglu_fp8", "moe_quantize_weights_fp8",
                 "moe_grouped_matmul_fp8")
