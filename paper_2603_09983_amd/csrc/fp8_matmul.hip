@@ -291,11 +291,12 @@ constexpr int kTile = 256, kTileThreads = 512;             // weight rows of a t
 constexpr int kTileBytes = kTile * kBlock;
 constexpr int kChunk = 4;                                  // blocks whose scales are fetched together
 constexpr int kChunkBytes = kChunk * (kTile + kWave) * 4;  // of the tokens, then of the two blocks of weight rows (and padding)
+constexpr int kTableInts = 2 * (kMaxC + 1) + kTileThreads / kWave;   // count_tiles: experts' first tiles and rows, the wavefronts' sums
 template <int J>   // tokens of a tile: 32 J
 struct TileSize {
     static constexpr int kTokens = 32 * J, kStage = kTileBytes + kTokens * kBlock;
-    static constexpr int kScales = 2 * kStage, kTable = kScales + 2 * kChunkBytes, kLds = kTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
-    static_assert(kLds <= kLdsBytes, "two stages, their scales, the experts' first tiles");
+    static constexpr int kScales = 2 * kStage, kTable = kScales + 2 * kChunkBytes, kLds = kTable + kTableInts * 4;
+    static_assert(kLds <= kLdsBytes, "two stages, their scales, the experts' tiles and rows");
 };
 
 // 16 (or 4) bytes a lane from base + at to LDS, lane after lane from `to` on.  Not waited for by the compiler: the loop counts.
@@ -308,22 +309,19 @@ __device__ __forceinline__ void fetch4(uint32_t to, uint32_t at, const void *bas
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(at), "s"(base) : "memory");
 }
 
-// first[e] = tiles of `tokens` rows of the experts before e, e = 0..E (all threads of a workgroup; E <= 2 * threads).  No more than
-// there can be where no expert's rows are another's too.
-__device__ __forceinline__ void count_tiles(int tokens, const int32_t *offsets, int M, int E, int32_t *first, int32_t *wave_sum)
+// table[e] = tiles of `tokens` rows of the experts before e, e = 0..E (all threads of a workgroup; E <= 2 * threads): no more than
+// there can be where no expert's rows are another's too.  Behind these, from kMaxC + 1 on, the experts' first rows: place_of reads them here,
+// for a read from memory would be waited for together with all that the tile kernels have on its way there.
+__device__ __forceinline__ void count_tiles(int tokens, const int32_t *offsets, int M, int E, int32_t *table)
 {
+    int32_t *const rows = table + kMaxC + 1, *const wave_sum = rows + kMaxC + 1;
     const int most = (M + tokens - 1) / tokens + (E < M ? E : M);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
-    int n[2];
+    int at[3], n[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int e = 2 * tid + i;
-        n[i] = 0;
-        if (e < E) {
-            const int rows = clamped(offsets[e + 1], M) - clamped(offsets[e], M);
-            n[i] = rows > 0 ? (rows + tokens - 1) / tokens : 0;
-        }
-    }
+    for (int i = 0; i < 3; ++i) at[i] = 2 * tid + i <= E ? clamped(offsets[2 * tid + i], M) : 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) n[i] = 2 * tid + i < E && at[i + 1] > at[i] ? (at[i + 1] - at[i] + tokens - 1) / tokens : 0;
     int up = n[0] + n[1];
     for (int d = 1; d < kWave; d <<= 1) {
         const int o = __shfl_up(up, d);
@@ -333,12 +331,14 @@ __device__ __forceinline__ void count_tiles(int tokens, const int32_t *offsets, 
     __syncthreads();
     int before = up - n[0] - n[1];
     for (int v = 0; v < w; ++v) before += wave_sum[v];
-    auto put = [&](int e, int v) {
-        if (e <= E) first[e] = v < most ? v : most;
+    auto put = [&](int e, int v, int row) {
+        if (e > E) return;
+        table[e] = v < most ? v : most;
+        rows[e] = row;
     };
-    put(2 * tid, before);
-    put(2 * tid + 1, before + n[0]);
-    if (tid == kTileThreads - 1) put(2 * kTileThreads, before + n[0] + n[1]);
+    put(2 * tid, before, at[0]);
+    put(2 * tid + 1, before + n[0], at[1]);
+    if (tid == kTileThreads - 1) put(2 * kTileThreads, before + n[0] + n[1], at[2]);
     __syncthreads();
 }
 
@@ -347,16 +347,15 @@ struct Place {
     int e, n0, r0, end;
 };
 template <int ROWS, int TOKENS>
-__device__ __forceinline__ Place place_of(const MatmulArgs &a, const int32_t *first, int tiles_n, int t)
+__device__ __forceinline__ Place place_of(int E, const int32_t *table, int tiles_n, int t)
 {
     const int lane = threadIdx.x & (kWave - 1);
     int e = -1;   // the last expert whose first tile is not behind t
-    for (int i = 0; i < a.E; i += kWave)
-        e += __popcll(__ballot(i + lane < a.E && first[i + lane < a.E ? i + lane : 0] * tiles_n <= t));
-    const int f = __builtin_amdgcn_readfirstlane(first[e]), m = __builtin_amdgcn_readfirstlane(first[e + 1]) - f;
-    const int local = t - f * tiles_n, n = local / m;
-    const int lo = clamped(a.offsets[e], a.M), hi = clamped(a.offsets[e + 1], a.M);
-    return Place{e, n * ROWS, lo + (local - n * m) * TOKENS, hi};
+    for (int i = 0; i < E; i += kWave)
+        e += __popcll(__ballot(i + lane < E && table[i + lane < E ? i + lane : 0] * tiles_n <= t));
+    auto entry = [&](int i) { return __builtin_amdgcn_readfirstlane(table[i]); };
+    const int f = entry(e), m = entry(e + 1) - f, local = t - f * tiles_n, n = local / m;
+    return Place{e, n * ROWS, entry(kMaxC + 1 + e) + (local - n * m) * TOKENS, entry(kMaxC + 2 + e)};
 }
 
 template <bool OUT16, bool EXACT, int J>
@@ -364,13 +363,13 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
 {
     constexpr int kTokens = TileSize<J>::kTokens, kStageBytes = TileSize<J>::kStage, kTileScales = TileSize<J>::kScales;
     extern __shared__ __align__(16) uint8_t lds[];
-    int32_t *first = (int32_t *)(lds + TileSize<J>::kTable);
+    int32_t *const table = (int32_t *)(lds + TileSize<J>::kTable);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock, tiles_n = (a.N + kTile - 1) / kTile, nb = (a.N + kBlock - 1) / kBlock;
-    count_tiles(kTokens, a.offsets, a.M, a.E, first, first + kMaxC + 1);
-    const int total = __builtin_amdgcn_readfirstlane(first[a.E]) * tiles_n;
+    count_tiles(kTokens, a.offsets, a.M, a.E, table);
+    const int total = __builtin_amdgcn_readfirstlane(table[a.E]) * tiles_n;
 
-    auto place = [&](int t) { return place_of<kTile, kTokens>(a, first, tiles_n, t); };
+    auto place = [&](int t) { return place_of<kTile, kTokens>(a.E, table, tiles_n, t); };
 
     // What this thread fetches of a step: rows tid / 8 + 64 i of both tiles, one 16-byte word each.
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
@@ -570,21 +569,21 @@ __global__ __launch_bounds__(kTileThreads) void tile_matmul_kernel(MatmulArgs a)
 constexpr int kRing = 4, kRingTile = 128;
 constexpr int kRingHalf = kRingTile * kBlock, kRingStage = 2 * kRingHalf;
 constexpr int kRingChunk = kChunk * (kRingTile + kWave) * 4, kRingScales = kRing * kRingStage;
-constexpr int kRingTable = kRingScales + kRing * kRingChunk, kRingLds = kRingTable + (kMaxC + 1 + kTileThreads / kWave) * 4;
-static_assert(kRingLds <= kLdsBytes, "the steps, their scales, the experts' first tiles");
+constexpr int kRingTable = kRingScales + kRing * kRingChunk, kRingLds = kRingTable + kTableInts * 4;
+static_assert(kRingLds <= kLdsBytes, "the steps, their scales, the experts' tiles and rows");
 
 template <bool OUT16, bool EXACT>
 __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    int32_t *first = (int32_t *)(lds + kRingTable);
+    int32_t *const table = (int32_t *)(lds + kRingTable);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int col = lane & 15, grp = lane >> 4, kb = a.K / kBlock, tiles_n = (a.N + kRingTile - 1) / kRingTile;
-    count_tiles(kRingTile, a.offsets, a.M, a.E, first, first + kMaxC + 1);
-    const int total = __builtin_amdgcn_readfirstlane(first[a.E]) * tiles_n;
+    count_tiles(kRingTile, a.offsets, a.M, a.E, table);
+    const int total = __builtin_amdgcn_readfirstlane(table[a.E]) * tiles_n;
     const int G = gridDim.x, xcds = G % 8 ? 1 : 8, b0 = (blockIdx.x % xcds) * (G / xcds) + blockIdx.x / xcds;
     if (b0 >= total) return;
-    auto place = [&](int t) { return place_of<kRingTile, kRingTile>(a, first, tiles_n, t); };
+    auto place = [&](int t) { return place_of<kRingTile, kRingTile>(a.E, table, tiles_n, t); };
 
     // The loads' walk over the steps of all tiles: two 16-byte words a thread of both operands, rows tid / 8 and 64 further on; the scales
     // of four blocks at a time, tokens' by wavefronts 0 and 1, the weights' by wavefront 2 (every lane the same).
