@@ -37,7 +37,7 @@ __device__ __forceinline__ void load16(const void *x, size_t row, int c, int K, 
 
 // e^x as 2^t, t = x log2(e), by the instruction, which is one step off at most.  What the roundings of t and of log2(e) have left out of the
 // exponent, up to 6e-6 at |x| = 87, comes back as a factor (the rounding of a product is a fused multiply-add).  Within four roundings of
-// 2^-24 where the result is a normal number.  Without the factor 59 roundings, with expf 39 us instead of the 31 of the call below.
+// 2^-24 where the result is a normal number; without the factor it was 59.  (With expf and a division the call below takes 39 us instead of 31.)
 __device__ __forceinline__ float exponential(float x)
 {
     constexpr double log2e = 1.4426950408889634, ln2 = 0.69314718055994531;
@@ -54,8 +54,8 @@ __device__ __forceinline__ float silu(float g)
 }
 
 // Eight lanes have a block, sixteen values a lane: the block's largest magnitude comes from three exchanges in registers, and a row is read
-// once.  24576 rows of SiLU(gate) * up, 1408 of each in bf16: 32 us, 5.4 TB/s.  (The exponential and the quotient in 32 bits; the only
-// rounding to fewer is that to e4m3.)
+// once.  24576 rows of SiLU(gate) * up, 1408 of each in bf16: 31 us, 5.6 TB/s.  (SiLU * up within nine roundings of 2^-24; the
+// only rounding to fewer bits is that to e4m3.)
 template <bool BF16, bool SWIGLU>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(QuantArgs a)
 {

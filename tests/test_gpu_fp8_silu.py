@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("up", [1.0, -3.0, 1e15])
 def test_silu_in_32_bits_over_the_range(up):
     """Gates from -87 to 87, one to a block, whose scale times 448 is then |silu(gate) * up|.  Off by: the
-    exponential's four roundings of 2^-24, those of 1 + e, the quotient, the product and the scale's quotient: eight."""
+    exponential's four roundings of 2^-24, that of 1 + e, two of its reciprocal, those of the two products and of the scale's quotient: ten."""
     n = 4096
     gate = torch.linspace(-87.0, 87.0, n)
     gate = torch.where(gate.abs() < 1e-3, torch.full_like(gate, 0.5), gate)
@@ -21,7 +21,7 @@ def test_silu_in_32_bits_over_the_range(up):
     B.moe_swiglu_fp8(x.cuda(), False, None, n, 128, q, scale)
     want = (gate.double() * torch.sigmoid(gate.double()) * torch.tensor(up).double()).abs().clamp(min=2.0 ** -100)
     off = ((scale.cpu().double()[:, 0] * 448 - want).abs() / want)
-    assert float(off.max()) <= 8 * R.U * (1 + 2.0 ** -20), float(off.max()) / R.U
+    assert float(off.max()) <= 10 * R.U * (1 + 2.0 ** -20), float(off.max()) / R.U
 
 
 def test_gates_beyond_the_range():
