@@ -330,8 +330,8 @@ int moe_pool_load(const void *store_gate, const void *store_up, const void *stor
  * expert products of their own.  None of the calls below uses the state of a
  * workspace, waits for another workgroup or synchronises: calls on different
  * streams may run at the same time (with a workspace each, where one is
- * taken), and each can be captured into a graph.  T*k, rows <= 2^30; sizes
- * beyond the limits are MOE_ERR_SHAPE.  Pointers to rows are 16-byte aligned,
+ * taken), and each can be captured into a graph.  T*k, rows <= 2^30, and as
+ * said with each call; sizes beyond the limits are MOE_ERR_SHAPE.  Pointers to rows are 16-byte aligned,
  * widths multiples of 8 (MOE_ERR_ALIGN).  Outputs do not overlap inputs.
  * x_bf16, rows_bf16, out_bf16, w_bf16: elements are bf16 (non-zero) or fp32
  * (0).  (moe_route_topk takes T*E <= 65536: a longer batch is routed in
@@ -345,7 +345,8 @@ int moe_pool_load(const void *store_gate, const void *store_up, const void *stor
  *                  ascending inside an expert; -1 from offsets[E] on;
  *   pos [T,k]      the row of an assignment, or -1.
  * workspace: moe_sort_workspace_bytes(T, k, E) bytes, 16-byte aligned, needs
- * no initialisation and holds nothing between calls. */
+ * no initialisation and holds nothing between calls (asked for whatever the
+ * sizes; written where T*k > 16384). */
 int moe_sort_workspace_bytes(int T, int k, int E, size_t *bytes_out);
 int moe_sort_assignments(const int32_t *ids, int T, int k, int E, int32_t *offsets, int32_t *order, int32_t *pos,
                          void *workspace, size_t workspace_bytes, void *stream);
@@ -353,18 +354,20 @@ int moe_sort_assignments(const int32_t *ids, int T, int k, int E, int32_t *offse
 /* Tokens' rows into sorted order: out[pos[t,j],:] = x[t,:].  x [T,H]; out
  * [R,H] of the same type; pos [T,k]: distinct rows, or values outside [0,R)
  * for assignments of no row.  Rows of `out` that pos does not name are left as
- * they were.  Its gradient is moe_unpermute with topk_w = NULL. */
+ * they were.  Its gradient is moe_unpermute with topk_w = NULL.
+ * T * ceil(H/2048) < 2^31 (bf16; fp32: H/1024). */
 int moe_permute(const void *x, int x_bf16, const int32_t *pos, int T, int k, int H, int R, void *out, void *stream);
 
 /* ... each row quantised on the way as by moe_quantize_fp8: q [R,Hp] e4m3,
- * scale [R,Hp/128]. */
+ * scale [R,Hp/128].  H <= 2^24, T * ceil(H/128) < 2^31. */
 int moe_permute_fp8(const void *x, int x_bf16, const int32_t *pos, int T, int k, int H, int R, void *q, float *scale,
                     void *stream);
 
 /* Back into token order:  out[t,:] (+)= sum over j of topk_w[t,j] rows[pos[t,j],:],
  * summed in fp32, j ascending; values of pos outside [0,R) add nothing.
  * rows [R,H]; topk_w [T,k] fp32 or NULL (all ones); out [T,H]; accumulate != 0
- * adds to what `out` holds (before the first j), else `out` is overwritten. */
+ * adds to what `out` holds (before the first j), else `out` is overwritten.
+ * T * ceil(H/512) < 2^31. */
 int moe_unpermute(const void *rows, int rows_bf16, const int32_t *pos, const float *topk_w, int T, int k, int H, int R,
                   void *out, int out_bf16, int accumulate, void *stream);
 
@@ -387,15 +390,18 @@ int moe_unpermute_backward(const void *dout, int dout_bf16, const void *rows, in
  *
  * Rows: x [M,K] -> q [M,Kp], scale [M,Kp/128], blocks of 128 of a row.
  * n_rows: device pointer to the number of rows that hold something (offsets + E
- * of a sort; clamped to [0,M]; later rows are left as they were), or NULL: M. */
+ * of a sort; clamped to [0,M]; later rows are left as they were), or NULL: M.
+ * M * ceil(K/128) < 2^31, here and in moe_swiglu_fp8 (F <= 2^24). */
 int moe_quantize_fp8(const void *x, int x_bf16, const int32_t *n_rows, int M, int K, void *q, float *scale, void *stream);
 
-/* ... of silu(gate) * up, computed in fp32: gate_up [M,2F] holds gate in the
- * first F columns, up in the others; q [M,Fp], scale [M,Fp/128]. */
+/* ... of silu(gate) * up, computed in fp32 (within nine roundings of 2^-24):
+ * gate_up [M,2F] holds gate in the first F columns, up in the others; q [M,Fp],
+ * scale [M,Fp/128]. */
 int moe_swiglu_fp8(const void *gate_up, int x_bf16, const int32_t *n_rows, int M, int F, void *q, float *scale, void *stream);
 
 /* Weights: w [E,N,K] -> q [E,N,Kp], scale [E,ceil(N/128),Kp/128], blocks of
- * 128 x 128 (fewer rows at the end of a matrix).  E <= 1024. */
+ * 128 x 128 (fewer rows at the end of a matrix).  E <= 1024, N <= 2^24,
+ * E * ceil(N/128) * ceil(K/128) < 2^31. */
 int moe_quantize_weights_fp8(const void *w, int w_bf16, int E, int N, int K, void *q, float *scale, void *stream);
 
 /* Products of sorted rows with their experts' weights:
@@ -412,10 +418,12 @@ int moe_quantize_weights_fp8(const void *w, int w_bf16, int E, int N, int K, voi
  * 2^-13 of the largest: off by 2e-5 of the results' norm on normally
  * distributed values, and by 7 * 2^-13 of the sum of the products' magnitudes
  * at most, which is not small beside a sum that cancels.  E <= 1024,
- * N <= 2^24, K <= 2^20; E = 1 with offsets {0, M} is the plain product.  The
- * gradient to x is the same call on the quantised gradient and the transposed
- * weights.  An element is the same from call to call; between calls of other
- * sizes the order of its sum may differ. */
+ * N <= 2^24, K <= 2^20, (ceil(M/128) + E) * ceil(N/128) < 2^30.  The two
+ * scales are multiplied first, in fp32: a product of theirs beyond 2^128 is
+ * infinite, one below 2^-126 keeps fewer bits.  E = 1 with offsets {0, M} is
+ * the plain product.  The gradient to x is the same call on the quantised
+ * gradient and the transposed weights.  An element is the same from call to
+ * call; between calls of other sizes the order of its sum may differ. */
 enum { MOE_BF16_SHORT_SUMS = 2 };   /* a value of out_bf16 */
 int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const void *w, const float *w_scale,
                            const int32_t *offsets, int M, int N, int K, int E, void *out, int out_bf16, void *stream);

@@ -824,13 +824,13 @@ extern "C" int moe_grouped_matmul_fp8(const void *x, const float *x_scale, const
 {
     if (!x || !x_scale || !w || !w_scale || !offsets || !out) return MOE_ERR_NULL;
     if (M < 1 || N < 1 || K < 1 || E < 1 || E > kMaxC || M > 1 << 30 || N > 1 << 24 || K > 1 << 20) return MOE_ERR_SHAPE;
+    if ((size_t)((M + 127) / 128 + E) * ((N + 127) / 128) >= (size_t)1 << 30) return MOE_ERR_SHAPE;
     if (N % 8 || K % kBlock || !aligned16(x) || !aligned16(w) || !aligned16(out)) return MOE_ERR_ALIGN;
     MatmulArgs a = {(const uint8_t *)x, (const uint8_t *)w, x_scale, w_scale, offsets, out, M, N, K, E,
                     K / kBlock % 4 == 0 && aligned16(x_scale) && aligned16(w_scale), 0};
     hipError_t err;
     const int cus = device_cus(&err);
     if (err != hipSuccess) return launch_failed(err);
-    if ((size_t)((M + 127) / 128 + E) * ((N + 127) / 128) >= (size_t)1 << 30) return MOE_ERR_SHAPE;
     const bool exact = out_bf16 != MOE_BF16_SHORT_SUMS;
     const Choice c = choose(M, N, K, E, exact, cus);
     auto tiles = [&](const void *fn, int rows, int tokens, int lds) {

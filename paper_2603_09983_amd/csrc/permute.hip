@@ -446,6 +446,7 @@ extern "C" int moe_permute_fp8(const void *x, int x_bf16, const int32_t *pos, in
     if (!x || !pos || !q || !scale) return MOE_ERR_NULL;
     int rc = check_rows(T, k, H, R);
     if (rc) return rc;
+    if (H > 1 << 24) return MOE_ERR_SHAPE;
     if (!aligned16(x) || !aligned16(q)) return MOE_ERR_ALIGN;
     MoveFp8Args a = {x, pos, (u32x4 *)q, scale, k, R, H, 0, (unsigned)((H + kBlock - 1) / kBlock), 0, 0};
     a.stream = (size_t)T * k * a.blocks * kBlock > kStreamBytes;
