@@ -1,6 +1,7 @@
 // C-ABI of libmoe_spac.so: argument checks and launch sequencing only.
 #include "../../include/moe_spac.h"
 #include "moe_internal.h"
+#include "rows_device.h"
 #include <mutex>
 #include <unordered_map>
 #include <vector>

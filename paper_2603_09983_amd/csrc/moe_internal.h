@@ -395,10 +395,6 @@ hipError_t launch_combine(const CombineArgs &a, hipStream_t s);
 hipError_t launch_clear_ctrl(void *workspace, size_t bytes, hipStream_t s);
 // a launch that the measurement aid times by the dispatch's own start and end stamps when enabled
 hipError_t launch_timed(const void *fn, dim3 grid, dim3 block, void **params, size_t lds, hipStream_t s, int kind);
-// one of the calls on rows (permute.hip, fp8.hip, fp8_matmul.hip): `args` is the kernel's one argument; returns a status code
-int launch_rows(const void *fn, dim3 grid, int threads, void *args, size_t lds, void *stream, int kind);
-int launch_failed(hipError_t e);   // keeps the error's text for moe_status_string, returns MOE_ERR_LAUNCH
-static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 // event bracketing for the measurement aid (no-ops unless enabled)
 // Per-device state of the library (each guarded by one mutex; any host thread may call):
 // compute units of the current device = workgroups of the chip-wide launches (capped at kMaxGroups; 0 and

@@ -1,8 +1,13 @@
-// What the kernels that move, sum and quantise rows share: 16-byte words of bf16 or fp32 as floats, and the 8-bit blocks.
+// What the calls that move, sum, quantise and multiply rows share: their launch, 16-byte words of bf16 or fp32 as floats, the 8-bit blocks.
 #pragma once
 #include "moe_internal.h"
 
 namespace moe {
+
+// Launch of one of the calls on rows (permute.hip, fp8.hip, fp8_matmul.hip): `args` is the kernel's one argument; returns a status code.
+int launch_rows(const void *fn, dim3 grid, int threads, void *args, size_t lds, void *stream, int kind);
+int launch_failed(hipError_t e);   // keeps the error's text for moe_status_string, returns MOE_ERR_LAUNCH
+static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 namespace rows {
 
