@@ -90,7 +90,8 @@ __device__ __forceinline__ f32x4 mfma128(const Operand<true> &a, const Operand<t
 // keeps nobody waiting: those of the first 32 go by the expert, the others are found from all counts.  (All of them found so: 128 rows
 // on 256 experts of 2048 x 1024 46 instead of 34 us.  Workgroups by the mean count, in turn over an expert's rows: 650 skewed rows on
 // 256 experts of 384 x 1088 33 instead of 13 us.)
-// 27 rows on 18 of 64 experts of 2816 x 2048: 18 us, 6.0 TB/s; 2 rows on 8 of 4096 x 14336: 20 us, 5.9 TB/s, launch included.
+// 27 rows on 18 of 64 experts of 2816 x 2048: 21 us, 5.1 TB/s; 2 rows on 8 of 4096 x 14336: 20 us, 5.8 TB/s, launch included.  (The
+// 8-bit instruction would take 7 % off the first and 1 % off the second: its sums are not offered here.)
 constexpr int kMostWaves = 8;
 
 // A load instruction takes eight rows' whole 128 columns (16 rows x 64 columns, as the matrix instruction has them, reach 5.8 TB/s, and
@@ -272,13 +273,13 @@ __global__ __launch_bounds__(kMostWaves *kWave) void stream_matmul_kernel(Matmul
 
 // ---- many rows to an expert: tiles of 256 weight rows x 256 tokens (or 128) through LDS ----
 // One workgroup of eight wavefronts per CU walks the tiles; a step is one block of 128 columns, 32 KB of weights and 32 (16) KB of rows.
-// A wavefront has 64 weight rows x 128 (64) tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core) four multiply-adds (16
-// cycles of the vector ALU) bring the block's sum, times its scales, into the tile's.
+// A wavefront has 64 weight rows x 128 (64) tokens: for each 16 x 16 x 128 product (32 cycles of the matrix core, 64 with 32-bit
+// sums) four multiply-adds (16 cycles of the vector ALU) bring the block's sum, times its scales, into the tile's.
 //
-// 49152 rows on 64 experts of 2816 x 2048, bf16 results: 577 us, 0.98 PFLOP/s, in tiles of 256 x 128; with short sums 329 us, 1.7 PFLOP/s,
+// 49152 rows on 64 experts of 2816 x 2048, bf16 results: 600 us, 0.95 PFLOP/s, in tiles of 256 x 128; with short sums 340 us, 1.7 PFLOP/s,
 // in tiles of 256 x 256.  There the products and multiply-adds alone, on random values, run at 3.1 (2.1 GHz); with the loads and stores
-// the clock is 1.7 GHz and the matrix cores are busy 44 % of the cycles, so that most of what is lost is waiting; one tile in seven has few
-// rows.
+// the clock is 1.7 GHz and the matrix cores are busy 43 % of the cycles (42 % at 1.9 GHz with 32-bit sums), so that most of what is lost is
+// waiting: two barriers a step keep the wavefronts together.  One tile in seven has few rows.
 //
 // LDS holds two steps.  A wavefront reads its weights of a step at its beginning and keeps them; once all have (a second barrier), the
 // weights of the step after next are requested into their place.  The rows of the next step are requested when everybody is through
@@ -765,8 +766,9 @@ __global__ __launch_bounds__(kTileThreads) void ring_matmul_kernel(MatmulArgs a)
 //      256 x 128 69/75     71/78     73/81     78/89     89/119    141/212   177/279   362/616      16/25     22/37     43/68     57/104
 //      256 x 256 72/-      73/-      76/-      80/-      90/-      117/-     191/-     335/-        20/-      31/-      55/-      84/-
 // (The others than streaming: tiles of weight rows x rows.  256 x 256 with 32-bit sums, whose operands are wider
-// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3000 calls of random sizes the choice took 1.025
-// times the fastest's time; without one of the kernels the fastest took 1.005 (256 x 256) to 1.14 (streaming) times as long as with all.
+// than its registers hold at once, was never the fastest by more than 5 %.)  Over 3000 calls of random sizes, short sums and
+// fp32 results, the choice took 1.025 times the fastest's time (bf16 results with 32-bit sums, 8388 other calls: 1.03);
+// without one of the kernels the fastest took 1.005 (256 x 256) to 1.14 (streaming) times as long as with all.
 //
 // All: the weights' bytes (at the rate that each reaches), once for each pass over an expert's rows.  The streaming kernel: what a CU
 // takes in, weights and rows, at 32 B/ns; or the blocks that a wavefront loads one after the other.  The tiles: rounds of them over the
